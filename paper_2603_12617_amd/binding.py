@@ -27,7 +27,8 @@ EXPORTS = ("oco_step_grid", "oco_paper_num_learners", "oco_workspace_bytes", "oc
            "oco_set_comparator", "oco_run_rounds", "oco_regret", "oco_get_state",
            "oco_cum_losses", "oco_accel_bounds", "oco_reset", "oco_set_timing", "oco_last_timing", "oco_last_kernel_timing",
            "oco_rounds_done", "oco_destroy", "oco_strerror",
-           "sd_verify", "sd_acceptance", "sd_strerror")
+           "sd_verify", "sd_acceptance", "sd_pages", "sd_cache_store", "sd_attend_workspace_bytes", "sd_attend",
+           "sd_verify_logits_workspace_bytes", "sd_verify_logits", "sd_strerror")
 
 
 class OcoConfig(C.Structure):
@@ -40,6 +41,31 @@ class OcoConfig(C.Structure):
 class OcoRounds(C.Structure):
     _fields_ = [("x", C.c_void_p), ("col", C.c_void_p), ("val", C.c_void_p), ("y", C.c_void_p),
                 ("x_run_stride", C.c_int64), ("y_run_stride", C.c_int64)]
+
+
+class SdPageStep(C.Structure):
+    _fields_ = ([(n, C.c_int64) for n in ("B", "page", "width", "table_stride", "pool", "tokens")]
+                + [(n, C.c_void_p) for n in ("pages", "length", "accepted", "add", "nfree", "table", "free", "pages_out",
+                                             "length_out", "kv_out", "nfree_out", "cu_out", "slot_out", "pos_out")])
+
+
+class SdCache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("pages", C.c_int64), ("page", C.c_int64), ("heads", C.c_int64), ("D", C.c_int64),
+                ("k_page_stride", C.c_int64), ("k_tok_stride", C.c_int64), ("k_head_stride", C.c_int64),
+                ("v_page_stride", C.c_int64), ("v_tok_stride", C.c_int64), ("v_head_stride", C.c_int64), ("dtype", C.c_int32)]
+
+
+class SdAttention(C.Structure):
+    _fields_ = [("cache", SdCache), ("B", C.c_int64), ("tokens", C.c_int64), ("Hq", C.c_int64), ("width", C.c_int64), ("table_stride", C.c_int64),
+                ("q", C.c_void_p), ("q_tok_stride", C.c_int64), ("q_head_stride", C.c_int64),
+                ("out", C.c_void_p), ("out_tok_stride", C.c_int64), ("out_head_stride", C.c_int64),
+                ("lse", C.c_void_p), ("cu", C.c_void_p), ("kv", C.c_void_p), ("table", C.c_void_p), ("window", C.c_int64), ("scale", C.c_double)]
+
+
+class SdLogits(C.Structure):
+    _fields_ = [("B", C.c_int64), ("rows", C.c_int64), ("V", C.c_int64), ("dtype", C.c_int32), ("p", C.c_void_p), ("p_stride", C.c_int64),
+                ("q", C.c_void_p), ("q_stride", C.c_int64), ("tok", C.c_void_p), ("r", C.c_void_p), ("noise", C.c_void_p),
+                ("noise_stride", C.c_int64), ("tau", C.c_void_p), ("cu", C.c_void_p)]
 
 
 class OcoError(RuntimeError):
@@ -100,6 +126,18 @@ def lib() -> C.CDLL:
         L.sd_verify.argtypes = [vp, vp, vp, vp, vp, i64, i64, i64, vp, vp, vp]
         L.sd_acceptance.restype = C.c_int
         L.sd_acceptance.argtypes = [vp, vp, i64, i64, i64, vp, vp]
+        L.sd_pages.restype = C.c_int
+        L.sd_pages.argtypes = [C.POINTER(SdPageStep), vp]
+        L.sd_cache_store.restype = C.c_int
+        L.sd_cache_store.argtypes = [C.POINTER(SdCache), vp, i64, i64, vp, i64, i64, vp, i64, vp]
+        L.sd_attend_workspace_bytes.restype = C.c_size_t
+        L.sd_attend_workspace_bytes.argtypes = [C.POINTER(SdAttention)]
+        L.sd_attend.restype = C.c_int
+        L.sd_attend.argtypes = [C.POINTER(SdAttention), vp, C.c_size_t, vp]
+        L.sd_verify_logits_workspace_bytes.restype = C.c_size_t
+        L.sd_verify_logits_workspace_bytes.argtypes = [C.POINTER(SdLogits)]
+        L.sd_verify_logits.restype = C.c_int
+        L.sd_verify_logits.argtypes = [C.POINTER(SdLogits), vp, vp, vp, C.c_size_t, vp]
         L.sd_strerror.restype = C.c_char_p
         L.sd_strerror.argtypes = [C.c_int]
         L.oco_rounds_done.restype = i64
@@ -376,3 +414,116 @@ def sd_acceptance(p, q, acc_out, stream=None) -> None:
     rc = lib().sd_acceptance(_dptr(p), _dptr(q), B, k, V, _dptr(acc_out), _stream_ptr(stream))
     if rc != 0:
         raise SdError(rc, "sd_acceptance")
+
+
+# ---------------------------------------------------------------------------
+# A served verification step (include/specdec.h): tables, cache, attention, verification from logits.
+# Tensors may be views: whatever strides the C ABI takes are passed on.
+_SD_DTYPE = {"torch.float32": 0, "torch.bfloat16": 1, "torch.float16": 2}
+
+
+def _sd_dtype(t) -> int:
+    d = _SD_DTYPE.get(str(t.dtype))
+    if d is None:
+        raise TypeError("float32, bfloat16 or float16 is wanted: got %s" % t.dtype)
+    return d
+
+
+def _want(t, name, dtype, *shape):
+    """Device address of an integer or float array of the step, whole and of the shape that the others imply."""
+    if str(t.dtype) != dtype or t.shape != shape or not t.is_cuda or not t.is_contiguous():
+        raise ValueError("%s: a contiguous %s GPU tensor of shape %s is wanted: got %s %s" % (name, dtype, list(shape), t.dtype, list(t.shape)))
+    return t.data_ptr()
+
+
+def _rows(t, name, dtype, *shape):
+    """Device address of a tensor whose last dimension is whole; the others may have any stride."""
+    if t.dtype != dtype or t.shape != shape or not t.is_cuda or (shape[-1] > 1 and t.stride(-1) != 1):
+        raise ValueError("%s: a %s GPU tensor of shape %s with whole rows is wanted: got %s %s" % (name, dtype, list(shape), t.dtype, list(t.shape)))
+    return t.data_ptr()
+
+
+_I32, _F32 = "torch.int32", "torch.float32"
+
+
+def sd_pages(pages, length, add, table, free, nfree, page, pages_out, length_out, kv_out, nfree_out, cu_out, slot_out, pos_out, *,
+             accepted=None, stream=None) -> None:
+    """Block tables and slot maps of a step.  pages, length, add, accepted [B] i32; table [B][width] i32 and free [pool] i32 are
+    updated in place; nfree, nfree_out [1]; pages_out, length_out, kv_out [B], cu_out [B+1], slot_out, pos_out [tokens] i32 are
+    written (tokens: the sum of add).  Asynchronous."""
+    B, width = table.shape
+    T, pool = slot_out.shape[0], free.shape[0]
+    step = SdPageStep(B, page, width, table.stride(0) if B > 1 else width, pool, T, _want(pages, "pages", _I32, B), _want(length, "length", _I32, B),
+                      None if accepted is None else _want(accepted, "accepted", _I32, B), _want(add, "add", _I32, B),
+                      _want(nfree, "nfree", _I32, 1), _rows(table, "table", nfree.dtype, B, width), _want(free, "free", _I32, pool),
+                      _want(pages_out, "pages_out", _I32, B), _want(length_out, "length_out", _I32, B), _want(kv_out, "kv_out", _I32, B),
+                      _want(nfree_out, "nfree_out", _I32, 1), _want(cu_out, "cu_out", _I32, B + 1), _want(slot_out, "slot_out", _I32, T),
+                      _want(pos_out, "pos_out", _I32, T))
+    rc = lib().sd_pages(C.byref(step), _stream_ptr(stream))
+    if rc != 0:
+        raise SdError(rc, "sd_pages")
+
+
+def _sd_cache(k_cache, v_cache) -> SdCache:
+    pages, page, heads, D = k_cache.shape
+    return SdCache(_rows(k_cache, "k_cache", k_cache.dtype, pages, page, heads, D), _rows(v_cache, "v_cache", k_cache.dtype, pages, page, heads, D),
+                   pages, page, heads, D, k_cache.stride(0), k_cache.stride(1), k_cache.stride(2), v_cache.stride(0), v_cache.stride(1),
+                   v_cache.stride(2), _sd_dtype(k_cache))
+
+
+def sd_cache_store(k, v, slot, k_cache, v_cache, stream=None) -> None:
+    """k, v [tokens][heads][D] into k_cache, v_cache [pages][page][heads][D] (any strides: a cache laid out head by head is its
+    transposed view) at slot [tokens] i32.  Asynchronous."""
+    c = _sd_cache(k_cache, v_cache)
+    T = slot.shape[0]
+    rc = lib().sd_cache_store(C.byref(c), _rows(k, "k", k_cache.dtype, T, c.heads, c.D), k.stride(0), k.stride(1),
+                              _rows(v, "v", k_cache.dtype, T, c.heads, c.D), v.stride(0), v.stride(1), _want(slot, "slot", _I32, T), T,
+                              _stream_ptr(stream))
+    if rc != 0:
+        raise SdError(rc, "sd_cache_store")
+
+
+def sd_attend_workspace_bytes(q, k_cache, table) -> int:
+    """Bytes of the workspace of sd_attend for these shapes; 0 if the call would be refused."""
+    pages, page, heads, D = k_cache.shape
+    (T, Hq, _), (B, width) = q.shape, table.shape
+    a = SdAttention(SdCache(None, None, pages, page, heads, D, 0, 0, 0, 0, 0, 0, _sd_dtype(k_cache)), B, T, Hq, width, width, None, 0, 0, None, 0, 0,
+                    None, None, None, None, 0, 1.0)
+    return int(lib().sd_attend_workspace_bytes(C.byref(a)))
+
+
+def sd_attend(q, k_cache, v_cache, cu, kv, table, out, scale, *, lse=None, window=0, ws, stream=None) -> None:
+    """Attention of q [tokens][Hq][D] over the pages of each request into out (of q's shape) and lse [tokens][Hq] f32; cu [B+1], kv [B],
+    table [B][width] i32 as sd_pages leaves them; ws: uint8 of sd_attend_workspace_bytes.  Asynchronous."""
+    c = _sd_cache(k_cache, v_cache)
+    (T, Hq, D), (B, width) = q.shape, table.shape
+    a = SdAttention(c, B, T, Hq, width, table.stride(0) if B > 1 else width, _rows(q, "q", k_cache.dtype, T, Hq, c.D), q.stride(0), q.stride(1),
+                    _rows(out, "out", k_cache.dtype, T, Hq, D), out.stride(0), out.stride(1),
+                    None if lse is None else _want(lse, "lse", _F32, T, Hq), _want(cu, "cu", _I32, B + 1), _want(kv, "kv", _I32, B),
+                    _rows(table, "table", cu.dtype, B, width), window, scale)
+    rc = lib().sd_attend(C.byref(a), _dptr(ws), ws.numel() * ws.element_size(), _stream_ptr(stream))
+    if rc != 0:
+        raise SdError(rc, "sd_attend")
+
+
+def sd_verify_logits_workspace_bytes(p, q, tau) -> int:
+    """Bytes of the workspace of sd_verify_logits for these shapes; 0 if the call would be refused.  q may be None."""
+    (T, V), B = p.shape, tau.shape[0]
+    a = SdLogits(B, T, V, _sd_dtype(p), None, V, 1 if q is not None else None, V, None, None, None, V, None, None)
+    return int(lib().sd_verify_logits_workspace_bytes(C.byref(a)))
+
+
+def sd_verify_logits(p, q, tok, r, noise, tau, cu, n_out, next_out, ws, stream=None) -> None:
+    """p [rows][V] logits of the target, q [rows-B][V] of the draft (None: drafts without a distribution), tok [rows-B] i32,
+    r [rows-B] f32, noise [B][V] f32, tau [B] f32, cu [B+1] i32 -> n_out, next_out [B] i32; ws: uint8 of
+    sd_verify_logits_workspace_bytes.  Asynchronous."""
+    (T, V), B = p.shape, tau.shape[0]
+    N = T - B
+    a = SdLogits(B, T, V, _sd_dtype(p), _rows(p, "p", p.dtype, T, V), p.stride(0) if T > 1 else V,
+                 None if q is None or N == 0 else _rows(q, "q", p.dtype, N, V), V if q is None or N < 2 else q.stride(0),
+                 _want(tok, "tok", _I32, N), _want(r, "r", _F32, N), _rows(noise, "noise", tau.dtype, B, V),
+                 noise.stride(0) if B > 1 else V, _want(tau, "tau", _F32, B), _want(cu, "cu", _I32, B + 1))
+    rc = lib().sd_verify_logits(C.byref(a), _want(n_out, "n_out", _I32, B), _want(next_out, "next_out", _I32, B), _dptr(ws),
+                                ws.numel() * ws.element_size(), _stream_ptr(stream))
+    if rc != 0:
+        raise SdError(rc, "sd_verify_logits")

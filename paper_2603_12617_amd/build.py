@@ -9,7 +9,8 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "liboco.so")
 SOURCES = ["oco_api.hip", "dense_rounds.hip", "sparse_rounds.hip", "meta.hip", "specdec.hip",
-           "comparator_gemm.hip", "dense_window.hip", "dense_split.hip", "dense_short.hip", "dense_run.hip"]
+           "comparator_gemm.hip", "dense_window.hip", "dense_split.hip", "dense_short.hip", "dense_run.hip",
+           "serve_pages.hip", "serve_store.hip", "serve_attend.hip", "verify_logits.hip"]
 FLAGS = ["-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-Wall",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 

@@ -301,6 +301,7 @@ const char *sd_strerror(int status)
         case SD_EINVAL: return "invalid argument";
         case SD_EUNSUPPORTED: return "size not supported by the kernels";
         case SD_EHIP: return "HIP runtime error";
+        case SD_ENOMEM: return "workspace too small";
         default: return "unknown status";
     }
 }
