@@ -1,7 +1,26 @@
 // Attention of a chunk of new tokens over a paged cache (sd_attend).
 //
-// One wavefront per (new token, query head).  Keys in blocks of 64, a key to a lane for the scores (float32 products
-// and sums over D), one pass with a running maximum and sum, then a share of D to a lane for the weighted values.
+// The rows of a request and key head are its (token, query head of the group) pairs, R = token * G + head, so the G
+// heads that share a key head share its keys' way through LDS.  A workgroup works a tile of rows over a range of keys in one
+// pass with a running maximum and sum per row.  Both products go through the 32x32x16 matrix instructions, transposed:
+//
+//   S^T (keys x rows)  = K Q^T     A: 32 keys from LDS, 16 bytes a lane;  B: 32 rows of q, in registers for the whole pass
+//   O^T (D x rows)    += V^T P^T   A: V from LDS, transposed by the read (ds_read_tr);  B: the weights
+//
+// A lane then holds 16 scores of ONE row (column lane & 31; the other half of its keys is in lane ^ 32): the maximum and
+// sum of a row are in-lane but for one exchange, the row's scale factors are a register of the lane, and the weights, rounded to
+// the cache's type, are already where the second product wants them: register r of half h is key
+// 8 (r >> 2) + 4 h + (r & 3) of 32, and since a sum over keys may take them in any order, the V operand is read in
+// that order.  Weights are not moved between lanes or through LDS.
+//
+// Keys and values go from the pages to LDS without passing registers (global_load_lds), one tile ahead of the products,
+// their 16-byte pieces permuted within a row (at the source, LDS order being fixed) so that the reads above find different banks.
+//
+// Two shapes of a workgroup:
+//   kRows wavefronts of 32 rows each over the same tile of 64 keys (prompts' chunks: bound by the matrix units), or
+//   one tile of 32 rows, and kKeys wavefronts with keys of their own that never wait for each other until they are joined in LDS at
+//   the end (decoding: bound by the cache's way from HBM; a wavefront has 16 KB of D = 128 on the way at any time).
+// Where tiles are few, the range of keys is split over workgroups, and a second kernel joins their parts.
 #include "../../include/specdec.h"
 
 #include <hip/hip_runtime.h>
@@ -10,67 +29,417 @@
 
 namespace {
 
-struct bf16 { uint16_t u; };
-__device__ __forceinline__ float to_float(bf16 v) { return __uint_as_float((unsigned)v.u << 16); }
-__device__ __forceinline__ float to_float(_Float16 v) { return (float)v; }
-__device__ __forceinline__ void from_float(float f, _Float16 &o) { o = (_Float16)f; }
-__device__ __forceinline__ void from_float(float f, bf16 &o)
+typedef unsigned int u2 __attribute__((ext_vector_type(2)));
+typedef unsigned int u4 __attribute__((ext_vector_type(4)));
+typedef float f16v __attribute__((ext_vector_type(16)));
+typedef float f2 __attribute__((ext_vector_type(2)));
+typedef short s4 __attribute__((ext_vector_type(4)));
+typedef short s8 __attribute__((ext_vector_type(8)));
+typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+typedef __bf16 b8 __attribute__((ext_vector_type(8)));
+typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+
+// ---- element types ----
+template <typename T> __device__ __forceinline__ f16v mfma(u4 a, u4 b, f16v c);
+template <> __device__ __forceinline__ f16v mfma<__bf16>(u4 a, u4 b, f16v c)
 {
-    const unsigned u = __float_as_uint(f);
-    o.u = f == f ? (uint16_t)((u + 0x7fffu + ((u >> 16) & 1u)) >> 16) : (uint16_t)0x7fc0;
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(b8, a), __builtin_bit_cast(b8, b), c, 0, 0, 0);
+}
+template <> __device__ __forceinline__ f16v mfma<_Float16>(u4 a, u4 b, f16v c)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(h8, a), __builtin_bit_cast(h8, b), c, 0, 0, 0);
+}
+// two floats rounded to nearest even
+template <typename T> __device__ __forceinline__ unsigned pack(float x, float y);
+template <> __device__ __forceinline__ unsigned pack<__bf16>(float x, float y) { const f2 f = {x, y}; return __builtin_bit_cast(unsigned, __builtin_convertvector(f, b2)); }
+template <> __device__ __forceinline__ unsigned pack<_Float16>(float x, float y) { const f2 f = {x, y}; return __builtin_bit_cast(unsigned, __builtin_convertvector(f, h2)); }
+
+// the value of lane ^ 32 and this lane's, in some order
+__device__ __forceinline__ f2 halves(float x)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return f2{__uint_as_float(r[0]), __uint_as_float(r[1])};
 }
 
-template <typename T> __global__ void __launch_bounds__(64) sd_attend_kernel(const sd_attention a)
+struct Attend {
+    sd_attention a;
+    int G, page_shift;             // query heads of a key head; key / page = mulhi(2 key, page_mul) >> page_shift
+    unsigned page_mul;
+    float scale;                   // scale * log2(e): weights are powers of two
+    int splits, row_tiles;         // of keys; tiles of rows there may be
+    float *part, *part_ml;         // [splits][tokens * Hq][D], [splits][tokens * Hq][2]: weighted values, (maximum, sum)
+};
+
+__device__ __forceinline__ int page_of(const Attend &p, int key) { return (int)(__umulhi(2u * (unsigned)key, p.page_mul) >> p.page_shift); }
+
+// 16 bytes a lane from `src` to LDS bytes to .. to + 1023 (lane by lane; lanes that are off leave theirs alone).  In assembly
+// because the compiler, which cannot tell the buffers apart, would wait for the loads of the next tile before the reads of this one; it
+// has no output registers, and whoever reads the bytes waits for vmcnt first.
+__device__ __forceinline__ void load_to_lds(const char *src, unsigned to)
 {
-    const int lane = threadIdx.x;
-    const int t = blockIdx.x, h = blockIdx.y, kh = h / (int)(a.Hq / a.cache.heads);
-    const int D = (int)a.cache.D, page = (int)a.cache.page;
-    int b = 0;
-    for (int n = (int)a.B; n > 1;) {
-        const int step = (n + 63) / 64;
-        const u_int64_t mask = __ballot(lane * step < n && a.cu[b + lane * step] <= t);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(src) : "memory");
+}
+__device__ __forceinline__ unsigned lds_address(const void *p) { return (unsigned)(uintptr_t)(const __attribute__((address_space(3))) void *)p; }
+
+// Tile x of all requests' rows: those of request b start at floor(cu[b] * G / tile) + b, which is known without a sum over
+// the requests and leaves every one as many as it needs.  Returns the request (by the lanes of a wavefront).
+__device__ __forceinline__ int request_of(const int32_t *cu, int B, int G, int tile, int x, int lane)
+{
+    int lo = 0, n = B;
+    while (n > 1) {
+        const int step = (n + 63) / 64, b = lo + lane * step;
+        const bool in = lane * step < n && (int)((unsigned)(cu[b] * G) / (unsigned)tile) + b <= x;
+        const unsigned long long mask = __ballot(in);
         const int last = mask ? 63 - __builtin_clzll(mask) : 0;
         n = min(step, n - last * step);
-        b += last * step;
+        lo += last * step;
     }
-    const int m = a.cu[b + 1] - a.cu[b];
-    const int64_t kv = min((int64_t)a.kv[b], a.width * page);
-    const int64_t pos = kv - m + (t - a.cu[b]);
-    const int64_t lo = a.window > 0 ? max((int64_t)0, pos - a.window + 1) : 0, hi = min(pos + 1, kv);
-    const T *q = static_cast<const T *>(a.q) + t * a.q_tok_stride + h * a.q_head_stride;
-    float top = -INFINITY, sum = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int64_t j0 = lo; j0 < hi; j0 += 64) {
-        const int64_t j = j0 + lane;
-        float s = -INFINITY;
-        int P = 0, at = 0;
-        if (j < hi) {
-            P = min(max(a.table[b * a.table_stride + j / page], 0), (int)a.cache.pages - 1);
-            at = (int)(j % page);
-            const T *k = static_cast<const T *>(a.cache.k) + P * a.cache.k_page_stride + at * a.cache.k_tok_stride + kh * a.cache.k_head_stride;
-            float d = 0.f;
-            for (int e = 0; e < D; ++e) d += to_float(q[e]) * to_float(k[e]);
-            s = d * (float)a.scale;
+    return lo;
+}
+
+struct Rows { int first, count, m, kv, before; };   // a request's first token, its tokens, keys, and keys before its first token (may be negative)
+__device__ __forceinline__ Rows rows_of(const sd_attention &a, int b)
+{
+    Rows r;
+    const int T = (int)a.tokens;
+    r.first = min(max(a.cu[b], 0), T);
+    r.m = min(max(a.cu[b + 1] - r.first, 0), T - r.first);
+    r.kv = (int)min((int64_t)max(a.kv[b], 0), a.width * a.cache.page);
+    r.before = r.kv - r.m;
+    r.count = r.m;
+    return r;
+}
+// the keys that a token of a request sees
+__device__ __forceinline__ int see_to(const Rows &r, int tok) { return min(max(r.before + tok + 1, 0), r.kv); }
+__device__ __forceinline__ int see_from(const sd_attention &a, const Rows &r, int tok)
+{
+    return a.window > 0 ? (int)min((int64_t)r.kv, max((int64_t)0, (int64_t)r.before + tok + 1 - a.window)) : 0;
+}
+
+// The steps (of `keys` keys) of a tile of rows, and those of one of its splits.
+struct Span { int first, count, per, used; };
+__device__ __forceinline__ Span span_of(const sd_attention &a, const Rows &r, int tok0, int tok1, int keys, int splits)
+{
+    Span s;
+    const int lo = see_from(a, r, tok0), hi = see_to(r, tok1);
+    s.first = lo / keys;
+    s.count = hi > lo ? (hi + keys - 1) / keys - s.first : 0;
+    s.per = max((s.count + splits - 1) / splits, 1);
+    s.used = (s.count + s.per - 1) / s.per;
+    return s;
+}
+
+template <int DK> struct Shape {
+    static constexpr int kPitch = DK <= 64 ? 128 : DK <= 128 ? 256 : 512;   // bytes of a row in LDS
+    static constexpr int kPieces = kPitch / 16;
+    static constexpr int kPerLoad = 64 / kPieces;                            // rows that one load of a wavefront brings
+    // where piece c of a row lies: a bijection of the row's pieces.  K is read 16 bytes a lane, eight lanes (rows) in a row
+    // of banks; V eight bytes a lane, four rows of 64 bytes together.
+    static __device__ __forceinline__ int k_at(int row, int c) { return c ^ (row & 7); }
+    static __device__ __forceinline__ int v_at(int row, int c) { return kPieces >= 16 ? c ^ (4 * (row & 3)) : c ^ (4 * ((row >> 1) & 1)); }
+};
+
+template <typename T, int DK, int kRows, int kKeys, int KT>
+__global__ void __launch_bounds__(64 * kRows * kKeys, kKeys > 1 && DK > 128 ? 1 : 2) sd_attend_kernel(const Attend p)
+{
+    static_assert(kRows == 1 || kKeys == 1, "wavefronts differ in rows or in keys");
+    typedef Shape<DK> S;
+    constexpr int kTile = KT * S::kPitch;                    // bytes of a tile of keys or values
+    constexpr int kLoads = KT / S::kPerLoad / kRows;         // of a wavefront, per tile and side
+    constexpr int kBlocks = KT / 32, kD = DK / 32, kQ = DK / 16;
+    constexpr int kBM = 32 * kRows;
+    extern __shared__ char lds[];
+    const sd_attention &a = p.a;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = kRows > 1 ? wave : 0, wk = kRows > 1 ? 0 : wave;
+    const int half = lane >> 5, col = lane & 31;
+    const int kh = blockIdx.x % (unsigned)a.cache.heads, x = p.row_tiles - 1 - (int)(blockIdx.x / (unsigned)a.cache.heads), split = blockIdx.y;   // (the rows with most keys first)
+    const int D = (int)a.cache.D, G = p.G, page = (int)a.cache.page;
+
+    const int b = request_of(a.cu, (int)a.B, G, kBM, x, lane);
+    const Rows rq = rows_of(a, b);
+    const int row0 = (x - ((int)((unsigned)(rq.first * G) / (unsigned)kBM) + b)) * kBM, rows = rq.m * G;
+    if (row0 < 0 || row0 >= rows) return;
+    const int tok0 = row0 / G, tok1 = (min(row0 + kBM, rows) - 1) / G;
+    const Span sp = span_of(a, rq, tok0, tok1, KT * kKeys, p.splits);
+    if (split >= max(sp.used, 1)) return;
+    const int t0 = (sp.first + split * sp.per) * kKeys + wk, t1 = (sp.first + min((split + 1) * sp.per, sp.count)) * kKeys;   // tiles t0, t0 + kKeys, .. < t1
+    const int first_key = see_from(a, rq, tok0), last_key = max(see_to(rq, tok1) - 1, 0);
+
+    // this lane's row
+    const int R = row0 + wm * 32 + col;
+    const bool there = R < rows;
+    const int tok = min(R, rows - 1) / G, head = kh * G + min(R, rows - 1) % G;
+    const int from = see_from(a, rq, tok), to = see_to(rq, tok);
+    // the wavefront's: keys in [whole_from, whole_to) are seen by all of its rows, those outside [any_from, any_to) by none
+    const int w0 = min(row0 + wm * 32, rows - 1) / G, w1 = min(row0 + wm * 32 + 31, rows - 1) / G;
+    const int any_from = see_from(a, rq, w0), whole_to = see_to(rq, w0), whole_from = see_from(a, rq, w1);
+    const int any_to = row0 + wm * 32 < rows ? see_to(rq, w1) : 0;
+
+    char *const kbuf = lds + wk * 4 * kTile, *const vbuf = kbuf + 2 * kTile;
+    if (D < DK) {                                            // pieces past D are never loaded
+        for (int i = tid; i < kKeys * 4 * kTile / 16; i += 64 * kRows * kKeys) reinterpret_cast<u4 *>(lds)[i] = u4{0, 0, 0, 0};
+        __syncthreads();
+    }
+
+    u4 q[kQ];
+    {
+        const T *src = static_cast<const T *>(a.q) + (int64_t)(rq.first + tok) * a.q_tok_stride + (int64_t)head * a.q_head_stride;
+#pragma unroll
+        for (int c = 0; c < kQ; ++c) {
+            const int d = 16 * c + 8 * half;
+            q[c] = d < D ? *reinterpret_cast<const u4 *>(src + d) : u4{0, 0, 0, 0};
         }
-        float most = s;
-        for (int sh = 32; sh >= 1; sh >>= 1) most = fmaxf(most, __shfl_xor(most, sh));
-        const float now = fmaxf(top, most), back = top == now ? 1.f : expf(top - now);
-        float w = j < hi && now > -INFINITY ? expf(s - now) : 0.f, all = w;
-        for (int sh = 32; sh >= 1; sh >>= 1) all += __shfl_xor(all, sh);
-        sum = sum * back + all;
+    }
+
+    // ---- from the pages to LDS: load i of a tile brings rows (i * kRows + wm) * kPerLoad + lane / kPieces ----
+    const int lrow = wm * S::kPerLoad + lane / S::kPieces, lpiece = lane % S::kPieces;
+    const char *const kbase = static_cast<const char *>(a.cache.k) + 2 * (int64_t)kh * a.cache.k_head_stride;
+    const char *const vbase = static_cast<const char *>(a.cache.v) + 2 * (int64_t)kh * a.cache.v_head_stride;
+    const int32_t *const table = a.table + (int64_t)b * a.table_stride;
+    int ids[kLoads];
+    // (places that none of the tile's rows sees get a key that one does see, so that a zero weight never meets what a page happens to hold)
+    auto key_of = [&](int t, int i) { return min(max(t * KT + i * kRows * S::kPerLoad + lrow, first_key), last_key); };
+    auto fetch_ids = [&](int t) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) ids[i] = table[page_of(p, key_of(t, i))];
+    };
+    const unsigned kto = __builtin_amdgcn_readfirstlane(lds_address(kbuf)), vto = __builtin_amdgcn_readfirstlane(lds_address(vbuf));
+    auto issue = [&](int t, int buf) {
+        const char *ks[kLoads], *vs[kLoads];
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int key = key_of(t, i), row = i * kRows * S::kPerLoad + lrow;
+            const int at = key - page_of(p, key) * page;
+            const int64_t id = min(max(ids[i], 0), (int)a.cache.pages - 1);
+            ks[i] = kbase + 2 * (id * a.cache.k_page_stride + at * a.cache.k_tok_stride) + 16 * S::k_at(row, lpiece);
+            vs[i] = vbase + 2 * (id * a.cache.v_page_stride + at * a.cache.v_tok_stride) + 16 * S::v_at(row, lpiece);
+        }
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const unsigned at = buf * kTile + (i * kRows + wm) * 1024;
+            if (D == DK) {
+                load_to_lds(ks[i], kto + at);
+                load_to_lds(vs[i], vto + at);
+            } else {
+                const int row = i * kRows * S::kPerLoad + lrow;
+                if (8 * S::k_at(row, lpiece) < D) load_to_lds(ks[i], kto + at);
+                if (8 * S::v_at(row, lpiece) < D) load_to_lds(vs[i], vto + at);
+            }
+        }
+    };
+
+    f16v o[kD];
+#pragma unroll
+    for (int d = 0; d < kD; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[d][r] = 0.f;
+    float top = -INFINITY, sum = 0.f;                        // of the row, powers of two; sum: of this half's keys
+
+    auto work = [&](int t, int buf) {
+        const int key0 = t * KT;
+        if (key0 >= any_to || key0 + KT <= any_from) return;
+        const char *kt = kbuf + buf * kTile, *vt = vbuf + buf * kTile;
+        f16v s[kBlocks];
+#pragma unroll
+        for (int n = 0; n < kBlocks; ++n) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[n][r] = 0.f;
+#pragma unroll
+            for (int c = 0; c < kQ; ++c) {
+                const int row = 32 * n + col;
+                s[n] = mfma<T>(*reinterpret_cast<const u4 *>(kt + row * S::kPitch + 16 * S::k_at(row, 2 * c + half)), q[c], s[n]);
+            }
+        }
+        if (key0 < whole_from || key0 + KT > whole_to) {
+#pragma unroll
+            for (int n = 0; n < kBlocks; ++n)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int key = key0 + 32 * n + 8 * (r >> 2) + 4 * half + (r & 3);
+                    s[n][r] = key >= from && key < to ? s[n][r] : -INFINITY;
+                }
+        }
+        float most = s[0][0];
+#pragma unroll
+        for (int n = 0; n < kBlocks; ++n)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) most = fmaxf(most, s[n][r]);
+        const f2 both = halves(most);
+        most = fmaxf(both[0], both[1]) * p.scale;
+        // the weights are taken relative to a maximum that lags behind by at most a factor of 2^8
+        if (__any(most > top + 8.f)) {
+            const float now = fmaxf(top, most), back = now == top ? 1.f : __builtin_amdgcn_exp2f(top - now);
+            top = now;
+            sum *= back;
+#pragma unroll
+            for (int d = 0; d < kD; ++d)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o[d][r] *= back;
+        }
+        const float ref = top == -INFINITY ? 0.f : top;
+        unsigned w[kBlocks][8];
+#pragma unroll
+        for (int n = 0; n < kBlocks; ++n)
+#pragma unroll
+            for (int r = 0; r < 16; r += 2) {
+                const float w0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][r], p.scale, -ref));
+                const float w1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][r + 1], p.scale, -ref));
+                sum += w0 + w1;
+                w[n][r / 2] = pack<T>(w0, w1);
+            }
+        // 16 keys at a time: this lane's are 16 c + 4 half + (0..3) and those + 8, at d = 32 dblock + col
+        const int vrow = 4 * half + ((lane & 15) >> 2), vpiece = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1), voff = 8 * (lane & 1);
+#pragma unroll
+        for (int n = 0; n < kBlocks; ++n)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                const u4 weights = {w[n][4 * c], w[n][4 * c + 1], w[n][4 * c + 2], w[n][4 * c + 3]};
+                const int r0 = 32 * n + 16 * c + vrow, r1 = r0 + 8;
+#pragma unroll
+                for (int d = 0; d < kD; ++d) {
+                    const char *x0 = vt + r0 * S::kPitch + 16 * S::v_at(r0, 4 * d + vpiece) + voff;
+                    const char *x1 = vt + r1 * S::kPitch + 16 * S::v_at(r1, 4 * d + vpiece) + voff;
+                    const u2 v0 = __builtin_bit_cast(u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4 *)x0));
+                    const u2 v1 = __builtin_bit_cast(u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4 *)x1));
+                    o[d] = mfma<T>(u4{v0[0], v0[1], v1[0], v1[1]}, weights, o[d]);
+                }
+            }
+    };
+
+    if (t0 < t1) {
+        fetch_ids(t0);
+        issue(t0, 0);
+        if (t0 + kKeys < t1) fetch_ids(t0 + kKeys);
+    }
+    int buf = 0;
+    for (int t = t0; t < t1; t += kKeys, buf ^= 1) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // tile t, and the pages of the next
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) asm volatile("" : "+v"(ids[i]));   // (nothing of them is waited for among the loads below)
+        if (kRows > 1) __syncthreads();                      // everyone's part of tile t is there, and tile t - 1 has been read
+        if (t + kKeys < t1) {
+            issue(t + kKeys, buf ^ 1);
+            if (t + 2 * kKeys < t1) fetch_ids(t + 2 * kKeys);
+        }
+        work(t, buf);
+    }
+    {
+        const f2 both = halves(sum);
+        sum = both[0] + both[1];
+    }
+
+    const bool whole = sp.used <= 1;
+    const int64_t orow = (int64_t)(rq.first + tok) * a.Hq + head;
+    if (kKeys > 1) {
+        // join the wavefronts: maximum, sum and values of each to LDS, then a share of D to each
+        constexpr int kP = DK + 4;                           // floats of a row
+        __syncthreads();
+        float *ml = reinterpret_cast<float *>(lds), *os = ml + kKeys * 64;
+        if (half == 0) { ml[wk * 64 + col] = top; ml[wk * 64 + 32 + col] = sum; }
+#pragma unroll
+        for (int d = 0; d < kD; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4)
+                *reinterpret_cast<float4 *>(os + (wk * 32 + col) * kP + 32 * d + 2 * r + 4 * half) = float4{o[d][r], o[d][r + 1], o[d][r + 2], o[d][r + 3]};
+        __syncthreads();
+        float now = -INFINITY, all = 0.f, part[kKeys];
+#pragma unroll
+        for (int k = 0; k < kKeys; ++k) now = fmaxf(now, ml[k * 64 + col]);
+#pragma unroll
+        for (int k = 0; k < kKeys; ++k) {
+            part[k] = ml[k * 64 + col] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[k * 64 + col] - now);
+            all += part[k] * ml[k * 64 + 32 + col];
+        }
         top = now;
-        for (int c = 0; c < 4; ++c) o[c] *= back;
-        const int n = (int)min((int64_t)64, hi - j0);
-        for (int i = 0; i < n; ++i) {
-            const float wi = __shfl(w, i);
-            const T *v = static_cast<const T *>(a.cache.v) + __shfl(P, i) * a.cache.v_page_stride + __shfl(at, i) * a.cache.v_tok_stride + kh * a.cache.v_head_stride;
-            for (int c = 0; c < 4; ++c)
-                if (c * 64 + lane < D) o[c] += wi * to_float(v[c * 64 + lane]);
+        sum = all;
+        constexpr int kShare = DK / kKeys / 2;               // of D, per half of a wavefront
+        const int d0 = (wk * 2 + half) * kShare;
+        const float inv = whole ? (sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum) : 1.f;
+        if (there) {
+#pragma unroll
+            for (int d = d0; d < d0 + kShare; d += 4) {
+                if (d >= D) break;
+                float4 v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int k = 0; k < kKeys; ++k) {
+                    const float4 e = *reinterpret_cast<const float4 *>(os + (k * 32 + col) * kP + d);
+                    if (part[k] != 0.f) { v.x += part[k] * e.x; v.y += part[k] * e.y; v.z += part[k] * e.z; v.w += part[k] * e.w; }
+                }
+                if (whole)
+                    *reinterpret_cast<u2 *>(static_cast<T *>(a.out) + (int64_t)(rq.first + tok) * a.out_tok_stride + (int64_t)head * a.out_head_stride + d) =
+                        u2{pack<T>(v.x * inv, v.y * inv), pack<T>(v.z * inv, v.w * inv)};
+                else
+                    *reinterpret_cast<float4 *>(p.part + ((int64_t)split * a.tokens * a.Hq + orow) * D + d) = v;
+            }
+        }
+    } else if (there) {
+        const float inv = whole ? (sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum) : 1.f;
+#pragma unroll
+        for (int d = 0; d < kD; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+                const int at = 32 * d + 2 * r + 4 * half;
+                if (at >= D) break;
+                if (whole)
+                    *reinterpret_cast<u2 *>(static_cast<T *>(a.out) + (int64_t)(rq.first + tok) * a.out_tok_stride + (int64_t)head * a.out_head_stride + at) =
+                        u2{pack<T>(o[d][r] * inv, o[d][r + 1] * inv), pack<T>(o[d][r + 2] * inv, o[d][r + 3] * inv)};
+                else
+                    *reinterpret_cast<float4 *>(p.part + ((int64_t)split * a.tokens * a.Hq + orow) * D + at) = float4{o[d][r], o[d][r + 1], o[d][r + 2], o[d][r + 3]};
+            }
+    }
+    if (there && half == 0 && wk == 0) {
+        if (whole) {
+            if (a.lse) a.lse[orow] = sum != 0.f ? (top + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f : -INFINITY;
+        } else {
+            float *ml = p.part_ml + 2 * ((int64_t)split * a.tokens * a.Hq + orow);
+            ml[0] = top; ml[1] = sum;
         }
     }
-    T *out = static_cast<T *>(a.out) + t * a.out_tok_stride + h * a.out_head_stride;
-    for (int c = 0; c < 4; ++c)
-        if (c * 64 + lane < D) from_float(sum > 0.f ? o[c] / sum : lo < hi ? o[c] : 0.f, out[c * 64 + lane]);
-    if (lane == 0 && a.lse) a.lse[t * a.Hq + h] = lo < hi ? top + logf(sum) : -INFINITY;
+}
+
+// The parts of rows whose keys were split: a wavefront per row, a share of D to a lane.
+template <typename T, int kBM, int kStep>
+__global__ void __launch_bounds__(256) sd_join_kernel(const Attend p)
+{
+    const sd_attention &a = p.a;
+    const int lane = threadIdx.x & 63;
+    const int64_t rows = a.tokens * a.Hq, orow = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (orow >= rows) return;
+    const int t = (int)(orow / a.Hq), head = (int)(orow % a.Hq), D = (int)a.cache.D;
+    int lo = 0, n = (int)a.B;
+    while (n > 1) {                                          // the last request with cu <= t
+        const int step = (n + 63) / 64;
+        const unsigned long long mask = __ballot(lane * step < n && a.cu[lo + lane * step] <= t);
+        const int last = mask ? 63 - __builtin_clzll(mask) : 0;
+        n = min(step, n - last * step);
+        lo += last * step;
+    }
+    const Rows rq = rows_of(a, lo);
+    const int R = (t - rq.first) * p.G + head % p.G, row0 = R / kBM * kBM;
+    if (t < rq.first || R >= rq.m * p.G) return;
+    const Span sp = span_of(a, rq, row0 / p.G, (min(row0 + kBM, rq.m * p.G) - 1) / p.G, kStep, p.splits);
+    if (sp.used <= 1) return;
+    float top = -INFINITY;
+    for (int s = 0; s < sp.used; ++s) top = fmaxf(top, p.part_ml[2 * (s * rows + orow)]);
+    float sum = 0.f;
+    float4 v{0.f, 0.f, 0.f, 0.f};
+    const int d = 4 * lane;
+    for (int s = 0; s < sp.used; ++s) {
+        const float m = p.part_ml[2 * (s * rows + orow)], w = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+        if (w == 0.f) continue;
+        sum += w * p.part_ml[2 * (s * rows + orow) + 1];
+        if (d < D) {
+            const float4 e = *reinterpret_cast<const float4 *>(p.part + (s * rows + orow) * D + d);
+            v.x += w * e.x; v.y += w * e.y; v.z += w * e.z; v.w += w * e.w;
+        }
+    }
+    const float inv = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;
+    if (d < D)
+        *reinterpret_cast<u2 *>(static_cast<T *>(a.out) + t * a.out_tok_stride + head * a.out_head_stride + d) =
+            u2{pack<T>(v.x * inv, v.y * inv), pack<T>(v.z * inv, v.w * inv)};
+    if (lane == 0 && a.lse) a.lse[orow] = sum != 0.f ? (top + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f : -INFINITY;
 }
 
 bool misaligned(const void *p, unsigned a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
@@ -80,19 +449,72 @@ int check(const sd_attention &a)
     const sd_cache &c = a.cache;
     if (a.B <= 0 || a.tokens < 0 || a.Hq <= 0 || a.width <= 0 || a.table_stride < a.width || a.window < 0) return SD_EINVAL;
     if (c.pages <= 0 || c.page <= 0 || c.heads <= 0 || c.D <= 0 || a.Hq % c.heads != 0) return SD_EINVAL;
-    if (!(a.scale > 0.0) || !(a.scale <= 3e38)) return SD_EINVAL;
+    if (!(a.scale > 0.0) || !(a.scale <= 1e30)) return SD_EINVAL;
     if (c.dtype != SD_F32 && c.dtype != SD_BF16 && c.dtype != SD_F16) return SD_EINVAL;
     const int64_t strides[] = {c.k_page_stride, c.k_tok_stride, c.k_head_stride, c.v_page_stride, c.v_tok_stride, c.v_head_stride,
                                a.q_tok_stride, a.q_head_stride, a.out_tok_stride, a.out_head_stride};
-    for (int64_t s : strides) {
-        if (s < 0) return SD_EINVAL;
-        if (s % 8 != 0) return SD_EINVAL;
-    }
+    for (int64_t s : strides)
+        if (s < 0 || s % 8 != 0) return SD_EINVAL;
     const int64_t most = 0x7fffffff;
     if (c.dtype == SD_F32 || c.D % 8 != 0 || c.D > SD_MAX_HEAD_DIM || a.B > SD_MAX_REQUESTS) return SD_EUNSUPPORTED;
-    if (c.pages > most || c.page > most || c.pages * c.page > most || a.width > most || a.width * c.page > most || a.Hq > 65535 || a.tokens * a.Hq > most)
+    if (c.pages > most || c.page > most || c.pages * c.page > most || a.width > most || a.width * c.page > most - 4096 ||
+        c.heads > most || a.tokens > most || a.Hq > most || a.tokens * a.Hq > most || a.Hq * a.B > most)
         return SD_EUNSUPPORTED;
     return SD_OK;
+}
+
+// ---- which kernel, and how many splits: by the shapes alone ----
+struct Plan { int dk, rows, step, tiles, splits; };   // rows of a tile, keys of a step
+Plan plan_of(const sd_attention &a)
+{
+    Plan p;
+    const int64_t G = a.Hq / a.cache.heads, D = a.cache.D, rows = a.tokens * G;
+    p.dk = D <= 64 ? 64 : D <= 96 ? 96 : D <= 128 ? 128 : D <= 192 ? 192 : 256;
+    const bool many = rows > 48 * a.B;
+    p.rows = many ? 128 : 32;
+    p.step = many ? (p.dk <= 128 ? 64 : 32) : (p.dk <= 128 ? 4 : 2) * 32;
+    p.tiles = (int)(rows / p.rows + a.B);
+    // enough workgroups for the chip, as far as the longest context allows
+    const int64_t there = (rows / p.rows > a.B ? rows / p.rows : a.B) * a.cache.heads;
+    int64_t longest = a.width * a.cache.page;
+    if (a.window > 0 && a.window + p.rows / G + 1 < longest) longest = a.window + p.rows / G + 1;
+    int64_t splits = there < 512 ? (1024 + there - 1) / there : 1;
+    const int64_t steps = (longest + p.step - 1) / p.step;
+    if (splits > steps) splits = steps;
+    if (splits > 256) splits = 256;
+    p.splits = (int)(splits < 1 ? 1 : splits);
+    return p;
+}
+size_t part_bytes(const sd_attention &a, const Plan &p) { return p.splits > 1 ? (size_t)p.splits * a.tokens * a.Hq * (a.cache.D + 2) * 4 : 0; }
+
+template <typename T, int DK> void launch(const Attend &p, const Plan &plan, hipStream_t st)
+{
+    const dim3 grid((unsigned)(p.a.cache.heads * plan.tiles), (unsigned)plan.splits);
+    const dim3 jgrid((unsigned)((p.a.tokens * p.a.Hq + 3) / 4));
+    constexpr int kPitch = Shape<DK>::kPitch, kKeys = DK <= 128 ? 4 : 2, KT = DK <= 128 ? 64 : 32;
+    if (plan.rows == 128) {
+        constexpr int bytes = 4 * KT * kPitch;
+        hipLaunchKernelGGL((sd_attend_kernel<T, DK, 4, 1, KT>), grid, dim3(256), bytes, st, p);
+        if (plan.splits > 1) hipLaunchKernelGGL((sd_join_kernel<T, 128, KT>), jgrid, dim3(256), 0, st, p);
+    } else {
+        constexpr int bytes = kKeys * 4 * 32 * kPitch;
+        static_assert(kKeys * (64 + 32 * (DK + 4)) * 4 <= bytes, "the join has room");
+        static const hipError_t once = hipFuncSetAttribute(reinterpret_cast<const void *>(sd_attend_kernel<T, DK, 1, kKeys, 32>),
+                                                           hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        (void)once;
+        hipLaunchKernelGGL((sd_attend_kernel<T, DK, 1, kKeys, 32>), grid, dim3(64 * kKeys), bytes, st, p);
+        if (plan.splits > 1) hipLaunchKernelGGL((sd_join_kernel<T, 32, 32 * kKeys>), jgrid, dim3(256), 0, st, p);
+    }
+}
+template <typename T> void launch(const Attend &p, const Plan &plan, hipStream_t st)
+{
+    switch (plan.dk) {
+        case 64: launch<T, 64>(p, plan, st); break;
+        case 96: launch<T, 96>(p, plan, st); break;
+        case 128: launch<T, 128>(p, plan, st); break;
+        case 192: launch<T, 192>(p, plan, st); break;
+        default: launch<T, 256>(p, plan, st); break;
+    }
 }
 
 }  // namespace
@@ -102,7 +524,7 @@ extern "C" {
 size_t sd_attend_workspace_bytes(const sd_attention *a)
 {
     if (!a || check(*a) != SD_OK) return 0;
-    return 16;
+    return 16 + part_bytes(*a, plan_of(*a));
 }
 
 int sd_attend(const sd_attention *args, void *ws, size_t ws_bytes, void *hip_stream)
@@ -116,12 +538,24 @@ int sd_attend(const sd_attention *args, void *ws, size_t ws_bytes, void *hip_str
     if (misaligned(a.cache.k, 16) || misaligned(a.cache.v, 16) || misaligned(a.q, 16) || misaligned(a.out, 16) || misaligned(a.lse, 4) ||
         misaligned(a.cu, 4) || misaligned(a.kv, 4) || misaligned(a.table, 4) || misaligned(ws, 16))
         return SD_EINVAL;
-    if (ws_bytes < sd_attend_workspace_bytes(args)) return SD_ENOMEM;
+    const Plan plan = plan_of(a);
+    if (ws_bytes < 16 + part_bytes(a, plan)) return SD_ENOMEM;
     if (a.tokens == 0) return SD_OK;
-    hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    const dim3 grid((unsigned)a.tokens, (unsigned)a.Hq);
-    if (a.cache.dtype == SD_BF16) hipLaunchKernelGGL(sd_attend_kernel<bf16>, grid, dim3(64), 0, st, a);
-    else hipLaunchKernelGGL(sd_attend_kernel<_Float16>, grid, dim3(64), 0, st, a);
+    Attend p;
+    p.a = a;
+    p.G = (int)(a.Hq / a.cache.heads);
+    p.scale = (float)(a.scale * 1.4426950408889634);
+    // key / page for keys below 2^31: with s = ceil(log2(page)), floor(key m / 2^(31 + s)), m = floor(2^(31 + s) / page) + 1 <= 2^32 - 1
+    int s = 0;
+    while ((1ll << s) < a.cache.page) ++s;
+    p.page_mul = (unsigned)((1ull << (31 + s)) / (unsigned long long)a.cache.page + 1);
+    p.page_shift = s;
+    p.splits = plan.splits;
+    p.row_tiles = plan.tiles;
+    p.part = static_cast<float *>(ws);
+    p.part_ml = p.part + (size_t)plan.splits * a.tokens * a.Hq * a.cache.D;
+    if (a.cache.dtype == SD_BF16) launch<__bf16>(p, plan, static_cast<hipStream_t>(hip_stream));
+    else launch<_Float16>(p, plan, static_cast<hipStream_t>(hip_stream));
     return hipGetLastError() == hipSuccess ? SD_OK : SD_EHIP;
 }
 
