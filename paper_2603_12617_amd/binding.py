@@ -419,31 +419,36 @@ def sd_acceptance(p, q, acc_out, stream=None) -> None:
 # ---------------------------------------------------------------------------
 # A served verification step (include/specdec.h): tables, cache, attention, verification from logits.
 # Tensors may be views: whatever strides the C ABI takes are passed on.
-_SD_DTYPE = {"torch.float32": 0, "torch.bfloat16": 1, "torch.float16": 2}
+# A call of a small step takes as long as its checks here, so these are few and plain: an array's type, its number of
+# entries, that it is whole and on the GPU.
+_SD_DTYPE = {}
+
+
+def _sd_types():
+    import torch
+    _SD_DTYPE.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2, "i32": torch.int32, "f32": torch.float32})
+    return _SD_DTYPE
 
 
 def _sd_dtype(t) -> int:
-    d = _SD_DTYPE.get(str(t.dtype))
+    d = (_SD_DTYPE or _sd_types()).get(t.dtype)
     if d is None:
         raise TypeError("float32, bfloat16 or float16 is wanted: got %s" % t.dtype)
     return d
 
 
-def _want(t, name, dtype, *shape):
-    """Device address of an integer or float array of the step, whole and of the shape that the others imply."""
-    if str(t.dtype) != dtype or t.shape != shape or not t.is_cuda or not t.is_contiguous():
-        raise ValueError("%s: a contiguous %s GPU tensor of shape %s is wanted: got %s %s" % (name, dtype, list(shape), t.dtype, list(t.shape)))
+def _want(t, name, dtype, n):
+    """Device address of an array of n entries."""
+    if t.dtype is not dtype or t.numel() != n or not t.is_contiguous() or not t.is_cuda:
+        raise ValueError("%s: a contiguous %s GPU tensor of %d entries is wanted: got %s %s" % (name, dtype, n, t.dtype, list(t.shape)))
     return t.data_ptr()
 
 
-def _rows(t, name, dtype, *shape):
+def _rows(t, name, dtype, shape):
     """Device address of a tensor whose last dimension is whole; the others may have any stride."""
-    if t.dtype != dtype or t.shape != shape or not t.is_cuda or (shape[-1] > 1 and t.stride(-1) != 1):
+    if t.dtype is not dtype or t.shape != shape or not t.is_cuda or (t.stride(-1) != 1 and shape[-1] > 1):
         raise ValueError("%s: a %s GPU tensor of shape %s with whole rows is wanted: got %s %s" % (name, dtype, list(shape), t.dtype, list(t.shape)))
     return t.data_ptr()
-
-
-_I32, _F32 = "torch.int32", "torch.float32"
 
 
 def sd_pages(pages, length, add, table, free, nfree, page, pages_out, length_out, kv_out, nfree_out, cu_out, slot_out, pos_out, *,
@@ -452,33 +457,36 @@ def sd_pages(pages, length, add, table, free, nfree, page, pages_out, length_out
     updated in place; nfree, nfree_out [1]; pages_out, length_out, kv_out [B], cu_out [B+1], slot_out, pos_out [tokens] i32 are
     written (tokens: the sum of add).  Asynchronous."""
     B, width = table.shape
-    T, pool = slot_out.shape[0], free.shape[0]
-    step = SdPageStep(B, page, width, table.stride(0) if B > 1 else width, pool, T, _want(pages, "pages", _I32, B), _want(length, "length", _I32, B),
-                      None if accepted is None else _want(accepted, "accepted", _I32, B), _want(add, "add", _I32, B),
-                      _want(nfree, "nfree", _I32, 1), _rows(table, "table", nfree.dtype, B, width), _want(free, "free", _I32, pool),
-                      _want(pages_out, "pages_out", _I32, B), _want(length_out, "length_out", _I32, B), _want(kv_out, "kv_out", _I32, B),
-                      _want(nfree_out, "nfree_out", _I32, 1), _want(cu_out, "cu_out", _I32, B + 1), _want(slot_out, "slot_out", _I32, T),
-                      _want(pos_out, "pos_out", _I32, T))
+    T, pool, i32 = slot_out.numel(), free.numel(), (_SD_DTYPE or _sd_types())["i32"]
+    step = SdPageStep(B, page, width, table.stride(0) if B > 1 else width, pool, T, _want(pages, "pages", i32, B), _want(length, "length", i32, B),
+                      None if accepted is None else _want(accepted, "accepted", i32, B), _want(add, "add", i32, B),
+                      _want(nfree, "nfree", i32, 1), _rows(table, "table", i32, (B, width)), _want(free, "free", i32, pool),
+                      _want(pages_out, "pages_out", i32, B), _want(length_out, "length_out", i32, B), _want(kv_out, "kv_out", i32, B),
+                      _want(nfree_out, "nfree_out", i32, 1), _want(cu_out, "cu_out", i32, B + 1), _want(slot_out, "slot_out", i32, T),
+                      _want(pos_out, "pos_out", i32, T))
     rc = lib().sd_pages(C.byref(step), _stream_ptr(stream))
     if rc != 0:
         raise SdError(rc, "sd_pages")
 
 
-def _sd_cache(k_cache, v_cache) -> SdCache:
-    pages, page, heads, D = k_cache.shape
-    return SdCache(_rows(k_cache, "k_cache", k_cache.dtype, pages, page, heads, D), _rows(v_cache, "v_cache", k_cache.dtype, pages, page, heads, D),
-                   pages, page, heads, D, k_cache.stride(0), k_cache.stride(1), k_cache.stride(2), v_cache.stride(0), v_cache.stride(1),
-                   v_cache.stride(2), _sd_dtype(k_cache))
+def _sd_cache(k_cache, v_cache):
+    """The cache's description, its type and its [heads][D]."""
+    shape = k_cache.shape
+    pages, page, heads, D = shape
+    dtype = k_cache.dtype
+    ks, vs = k_cache.stride(), v_cache.stride()
+    return SdCache(_rows(k_cache, "k_cache", dtype, shape), _rows(v_cache, "v_cache", dtype, shape), pages, page, heads, D, ks[0], ks[1], ks[2],
+                   vs[0], vs[1], vs[2], _sd_dtype(k_cache)), dtype, heads, D
 
 
 def sd_cache_store(k, v, slot, k_cache, v_cache, stream=None) -> None:
     """k, v [tokens][heads][D] into k_cache, v_cache [pages][page][heads][D] (any strides: a cache laid out head by head is its
     transposed view) at slot [tokens] i32.  Asynchronous."""
-    c = _sd_cache(k_cache, v_cache)
-    T = slot.shape[0]
-    rc = lib().sd_cache_store(C.byref(c), _rows(k, "k", k_cache.dtype, T, c.heads, c.D), k.stride(0), k.stride(1),
-                              _rows(v, "v", k_cache.dtype, T, c.heads, c.D), v.stride(0), v.stride(1), _want(slot, "slot", _I32, T), T,
-                              _stream_ptr(stream))
+    c, dtype, heads, D = _sd_cache(k_cache, v_cache)
+    T = slot.numel()
+    shape, ks, vs = (T, heads, D), k.stride(), v.stride()
+    rc = lib().sd_cache_store(C.byref(c), _rows(k, "k", dtype, shape), ks[0], ks[1], _rows(v, "v", dtype, shape), vs[0], vs[1],
+                              _want(slot, "slot", _SD_DTYPE["i32"], T), T, _stream_ptr(stream))
     if rc != 0:
         raise SdError(rc, "sd_cache_store")
 
@@ -495,12 +503,15 @@ def sd_attend_workspace_bytes(q, k_cache, table) -> int:
 def sd_attend(q, k_cache, v_cache, cu, kv, table, out, scale, *, lse=None, window=0, ws, stream=None) -> None:
     """Attention of q [tokens][Hq][D] over the pages of each request into out (of q's shape) and lse [tokens][Hq] f32; cu [B+1], kv [B],
     table [B][width] i32 as sd_pages leaves them; ws: uint8 of sd_attend_workspace_bytes.  Asynchronous."""
-    c = _sd_cache(k_cache, v_cache)
-    (T, Hq, D), (B, width) = q.shape, table.shape
-    a = SdAttention(c, B, T, Hq, width, table.stride(0) if B > 1 else width, _rows(q, "q", k_cache.dtype, T, Hq, c.D), q.stride(0), q.stride(1),
-                    _rows(out, "out", k_cache.dtype, T, Hq, D), out.stride(0), out.stride(1),
-                    None if lse is None else _want(lse, "lse", _F32, T, Hq), _want(cu, "cu", _I32, B + 1), _want(kv, "kv", _I32, B),
-                    _rows(table, "table", cu.dtype, B, width), window, scale)
+    c, dtype, heads, D = _sd_cache(k_cache, v_cache)
+    shape, (B, width) = q.shape, table.shape
+    T, Hq, Dq = shape
+    if Dq != D:
+        raise ValueError("q has heads of %d, the cache of %d" % (Dq, D))
+    i32, qs, os = _SD_DTYPE["i32"], q.stride(), out.stride()
+    a = SdAttention(c, B, T, Hq, width, table.stride(0) if B > 1 else width, _rows(q, "q", dtype, shape), qs[0], qs[1],
+                    _rows(out, "out", dtype, shape), os[0], os[1], None if lse is None else _want(lse, "lse", _SD_DTYPE["f32"], T * Hq),
+                    _want(cu, "cu", i32, B + 1), _want(kv, "kv", i32, B), _rows(table, "table", i32, (B, width)), window, scale)
     rc = lib().sd_attend(C.byref(a), _dptr(ws), ws.numel() * ws.element_size(), _stream_ptr(stream))
     if rc != 0:
         raise SdError(rc, "sd_attend")
@@ -517,13 +528,16 @@ def sd_verify_logits(p, q, tok, r, noise, tau, cu, n_out, next_out, ws, stream=N
     """p [rows][V] logits of the target, q [rows-B][V] of the draft (None: drafts without a distribution), tok [rows-B] i32,
     r [rows-B] f32, noise [B][V] f32, tau [B] f32, cu [B+1] i32 -> n_out, next_out [B] i32; ws: uint8 of
     sd_verify_logits_workspace_bytes.  Asynchronous."""
-    (T, V), B = p.shape, tau.shape[0]
-    N = T - B
-    a = SdLogits(B, T, V, _sd_dtype(p), _rows(p, "p", p.dtype, T, V), p.stride(0) if T > 1 else V,
-                 None if q is None or N == 0 else _rows(q, "q", p.dtype, N, V), V if q is None or N < 2 else q.stride(0),
-                 _want(tok, "tok", _I32, N), _want(r, "r", _F32, N), _rows(noise, "noise", tau.dtype, B, V),
-                 noise.stride(0) if B > 1 else V, _want(tau, "tau", _F32, B), _want(cu, "cu", _I32, B + 1))
-    rc = lib().sd_verify_logits(C.byref(a), _want(n_out, "n_out", _I32, B), _want(next_out, "next_out", _I32, B), _dptr(ws),
+    (T, V), B, dtype = p.shape, tau.numel(), p.dtype
+    N, d = T - B, _sd_dtype(p)
+    i32, f32 = _SD_DTYPE["i32"], _SD_DTYPE["f32"]
+    if q is not None and N == 0:
+        q = None
+    a = SdLogits(B, T, V, d, _rows(p, "p", dtype, (T, V)), p.stride(0) if T > 1 else V,
+                 None if q is None else _rows(q, "q", dtype, (N, V)), V if N < 2 or q is None else q.stride(0),
+                 _want(tok, "tok", i32, N), _want(r, "r", f32, N), _rows(noise, "noise", f32, (B, V)),
+                 noise.stride(0) if B > 1 else V, _want(tau, "tau", f32, B), _want(cu, "cu", i32, B + 1))
+    rc = lib().sd_verify_logits(C.byref(a), _want(n_out, "n_out", i32, B), _want(next_out, "next_out", i32, B), _dptr(ws),
                                 ws.numel() * ws.element_size(), _stream_ptr(stream))
     if rc != 0:
         raise SdError(rc, "sd_verify_logits")

@@ -67,8 +67,10 @@ struct Attend {
     int G, page_shift;             // query heads of a key head; key / page = mulhi(2 key, page_mul) >> page_shift
     unsigned page_mul;
     float scale;                   // scale * log2(e): weights are powers of two
-    int splits, row_tiles;         // of keys; tiles of rows there may be
+    int splits, min_steps;         // of keys; steps that a split has at least
+    int row_tiles;                 // tiles of rows there may be
     float *part, *part_ml;         // [splits][tokens * Hq][D], [splits][tokens * Hq][2]: weighted values, (maximum, sum)
+    int *used;                     // [tokens * Hq] parts of a row
 };
 
 __device__ __forceinline__ int page_of(const Attend &p, int key) { return (int)(__umulhi(2u * (unsigned)key, p.page_mul) >> p.page_shift); }
@@ -119,16 +121,18 @@ __device__ __forceinline__ int see_from(const sd_attention &a, const Rows &r, in
 
 // The steps (of `keys` keys) of a tile of rows, and those of one of its splits.
 struct Span { int first, count, per, used; };
-__device__ __forceinline__ Span span_of(const sd_attention &a, const Rows &r, int tok0, int tok1, int keys, int splits)
+__device__ __forceinline__ Span span_of(const sd_attention &a, const Rows &r, int tok0, int tok1, int keys, int splits, int min_steps)
 {
     Span s;
     const int lo = see_from(a, r, tok0), hi = see_to(r, tok1);
     s.first = lo / keys;
     s.count = hi > lo ? (hi + keys - 1) / keys - s.first : 0;
-    s.per = max((s.count + splits - 1) / splits, 1);
+    s.per = max((s.count + splits - 1) / splits, min_steps);
     s.used = (s.count + s.per - 1) / s.per;
     return s;
 }
+
+constexpr int kIds = 256;          // page ids that a wavefront keeps
 
 template <int DK> struct Shape {
     static constexpr int kPitch = DK <= 64 ? 128 : DK <= 128 ? 256 : 512;   // bytes of a row in LDS
@@ -141,9 +145,10 @@ template <int DK> struct Shape {
 };
 
 template <typename T, int DK, int kRows, int kKeys, int KT>
-__global__ void __launch_bounds__(64 * kRows * kKeys, kKeys > 1 && DK > 128 ? 1 : 2) sd_attend_kernel(const Attend p)
+__global__ void __launch_bounds__(64 * kRows * kKeys, kRows == 1 && DK > 128 ? 1 : 2) sd_attend_kernel(const Attend p)
 {
     static_assert(kRows == 1 || kKeys == 1, "wavefronts differ in rows or in keys");
+    constexpr bool kOwn = kRows == 1;                        // a wavefront has keys of its own
     typedef Shape<DK> S;
     constexpr int kTile = KT * S::kPitch;                    // bytes of a tile of keys or values
     constexpr int kLoads = KT / S::kPerLoad / kRows;         // of a wavefront, per tile and side
@@ -162,7 +167,7 @@ __global__ void __launch_bounds__(64 * kRows * kKeys, kKeys > 1 && DK > 128 ? 1 
     const int row0 = (x - ((int)((unsigned)(rq.first * G) / (unsigned)kBM) + b)) * kBM, rows = rq.m * G;
     if (row0 < 0 || row0 >= rows) return;
     const int tok0 = row0 / G, tok1 = (min(row0 + kBM, rows) - 1) / G;
-    const Span sp = span_of(a, rq, tok0, tok1, KT * kKeys, p.splits);
+    const Span sp = span_of(a, rq, tok0, tok1, KT * kKeys, p.splits, p.min_steps);
     if (split >= max(sp.used, 1)) return;
     const int t0 = (sp.first + split * sp.per) * kKeys + wk, t1 = (sp.first + min((split + 1) * sp.per, sp.count)) * kKeys;   // tiles t0, t0 + kKeys, .. < t1
     const int first_key = see_from(a, rq, tok0), last_key = max(see_to(rq, tok1) - 1, 0);
@@ -198,31 +203,28 @@ __global__ void __launch_bounds__(64 * kRows * kKeys, kKeys > 1 && DK > 128 ? 1 
     const char *const kbase = static_cast<const char *>(a.cache.k) + 2 * (int64_t)kh * a.cache.k_head_stride;
     const char *const vbase = static_cast<const char *>(a.cache.v) + 2 * (int64_t)kh * a.cache.v_head_stride;
     const int32_t *const table = a.table + (int64_t)b * a.table_stride;
-    int ids[kLoads];
     // (places that none of the tile's rows sees get a key that one does see, so that a zero weight never meets what a page happens to hold)
-    auto key_of = [&](int t, int i) { return min(max(t * KT + i * kRows * S::kPerLoad + lrow, first_key), last_key); };
-    auto fetch_ids = [&](int t) {
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) ids[i] = table[page_of(p, key_of(t, i))];
-    };
+    auto key_in = [&](int key) { return min(max(key, first_key), last_key); };
+    auto key_of = [&](int t, int i) { return key_in(t * KT + i * kRows * S::kPerLoad + lrow); };
     const unsigned kto = __builtin_amdgcn_readfirstlane(lds_address(kbuf)), vto = __builtin_amdgcn_readfirstlane(lds_address(vbuf));
-    auto issue = [&](int t, int buf) {
+    auto issue = [&](int t, int buf, auto page_id) {
         const char *ks[kLoads], *vs[kLoads];
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-            const int key = key_of(t, i), row = i * kRows * S::kPerLoad + lrow;
-            const int at = key - page_of(p, key) * page;
-            const int64_t id = min(max(ids[i], 0), (int)a.cache.pages - 1);
+            const int key = key_of(t, i), row = i * kRows * S::kPerLoad + lrow, place = page_of(p, key);
+            const int at = key - place * page;
+            const int64_t id = min(max(page_id(i, place), 0), (int)a.cache.pages - 1);
             ks[i] = kbase + 2 * (id * a.cache.k_page_stride + at * a.cache.k_tok_stride) + 16 * S::k_at(row, lpiece);
             vs[i] = vbase + 2 * (id * a.cache.v_page_stride + at * a.cache.v_tok_stride) + 16 * S::v_at(row, lpiece);
         }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // what was read from the buffer is there
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             const unsigned at = buf * kTile + (i * kRows + wm) * 1024;
             if (D == DK) {
                 load_to_lds(ks[i], kto + at);
                 load_to_lds(vs[i], vto + at);
-            } else {
+            } else {                                         // (every row has a piece below D, so every load is issued)
                 const int row = i * kRows * S::kPerLoad + lrow;
                 if (8 * S::k_at(row, lpiece) < D) load_to_lds(ks[i], kto + at);
                 if (8 * S::v_at(row, lpiece) < D) load_to_lds(vs[i], vto + at);
@@ -268,9 +270,10 @@ __global__ void __launch_bounds__(64 * kRows * kKeys, kKeys > 1 && DK > 128 ? 1 
             for (int r = 0; r < 16; ++r) most = fmaxf(most, s[n][r]);
         const f2 both = halves(most);
         most = fmaxf(both[0], both[1]) * p.scale;
-        // the weights are taken relative to a maximum that lags behind by at most a factor of 2^8
-        if (__any(most > top + 8.f)) {
-            const float now = fmaxf(top, most), back = now == top ? 1.f : __builtin_amdgcn_exp2f(top - now);
+        // the weights are taken relative to a maximum that lags behind by at most a factor of 2^8 (row by row: what a row gets does not depend on its neighbours)
+        const bool behind = most > top + 8.f;
+        if (__any(behind)) {
+            const float now = behind ? most : top, back = behind ? __builtin_amdgcn_exp2f(top - now) : 1.f;
             top = now;
             sum *= back;
 #pragma unroll
@@ -308,22 +311,55 @@ __global__ void __launch_bounds__(64 * kRows * kKeys, kKeys > 1 && DK > 128 ? 1 
             }
     };
 
-    if (t0 < t1) {
-        fetch_ids(t0);
-        issue(t0, 0);
-        if (t0 + kKeys < t1) fetch_ids(t0 + kKeys);
-    }
-    int buf = 0;
-    for (int t = t0; t < t1; t += kKeys, buf ^= 1) {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // tile t, and the pages of the next
+    if (kOwn) {
+        // Two tiles on the way.  The wavefront's page ids lie in LDS, kIds of them at a time: a load to registers would be waited for together with
+        // the tiles behind it.
+        int *const ids = reinterpret_cast<int *>(lds + kKeys * 4 * kTile) + wk * kIds;
+        const int last_place = page_of(p, last_key);
+        int ids_from = -kIds;
+        auto fetch = [&](int t, int buf) {
+            const int p0 = page_of(p, key_in(t * KT)), p1 = page_of(p, key_in(t * KT + KT - 1));
+            if (p0 < ids_from || p1 >= ids_from + kIds) {
+                ids_from = p0;
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) asm volatile("" : "+v"(ids[i]));   // (nothing of them is waited for among the loads below)
-        if (kRows > 1) __syncthreads();                      // everyone's part of tile t is there, and tile t - 1 has been read
-        if (t + kKeys < t1) {
-            issue(t + kKeys, buf ^ 1);
-            if (t + 2 * kKeys < t1) fetch_ids(t + 2 * kKeys);
+                for (int i = 0; i < kIds; i += 64) ids[i + lane] = table[min(p0 + i + lane, last_place)];
+            }
+            issue(t, buf, [&](int, int place) { return ids[place - ids_from]; });
+        };
+        if (t0 < t1) fetch(t0, 0);
+        if (t0 + kKeys < t1) fetch(t0 + kKeys, 1);
+        int buf = 0;
+        for (int t = t0; t < t1; t += kKeys, buf ^= 1) {
+            if (t + kKeys < t1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * kLoads) : "memory");   // all but the loads of the next tile
+            else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            work(t, buf);
+            if (t + 2 * kKeys < t1) fetch(t + 2 * kKeys, buf);
         }
-        work(t, buf);
+    } else {
+        // One tile on the way, and the page ids of the one behind it
+        int ids[kLoads];
+        auto fetch_ids = [&](int t) {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) ids[i] = table[page_of(p, key_of(t, i))];
+        };
+        auto id_of = [&](int i, int) { return ids[i]; };
+        if (t0 < t1) {
+            fetch_ids(t0);
+            issue(t0, 0, id_of);
+            if (t0 + 1 < t1) fetch_ids(t0 + 1);
+        }
+        int buf = 0;
+        for (int t = t0; t < t1; ++t, buf ^= 1) {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); // tile t, and the pages of the next
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) asm volatile("" : "+v"(ids[i]));   // (nothing of them is waited for among the loads below)
+            __syncthreads();                                 // everyone's part of tile t is there, and tile t - 1 has been read
+            if (t + 1 < t1) {
+                issue(t + 1, buf ^ 1, id_of);
+                if (t + 2 < t1) fetch_ids(t + 2);
+            }
+            work(t, buf);
+        }
     }
     {
         const f2 both = halves(sum);
@@ -390,6 +426,7 @@ __global__ void __launch_bounds__(64 * kRows * kKeys, kKeys > 1 && DK > 128 ? 1 
             }
     }
     if (there && half == 0 && wk == 0) {
+        if (p.splits > 1 && split == 0) p.used[orow] = sp.used;
         if (whole) {
             if (a.lse) a.lse[orow] = sum != 0.f ? (top + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f : -INFINITY;
         } else {
@@ -399,47 +436,57 @@ __global__ void __launch_bounds__(64 * kRows * kKeys, kKeys > 1 && DK > 128 ? 1 
     }
 }
 
-// The parts of rows whose keys were split: a wavefront per row, a share of D to a lane.
-template <typename T, int kBM, int kStep>
-__global__ void __launch_bounds__(256) sd_join_kernel(const Attend p)
+// The parts of rows whose keys were split: kLanes lanes a row (a workgroup, or a wavefront where parts are few), D / 4 of them to a
+// part.  Their number was left by the workgroups of the first split, so that nothing of the requests is looked up again.
+template <typename T, int kLanes> __global__ void __launch_bounds__(256) sd_join_kernel(const Attend p)
 {
+    constexpr int kRows = 256 / kLanes;
+    __shared__ float w_sh[kRows][256];
+    __shared__ float4 v_sh[kRows][kLanes];
     const sd_attention &a = p.a;
-    const int lane = threadIdx.x & 63;
-    const int64_t rows = a.tokens * a.Hq, orow = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (orow >= rows) return;
-    const int t = (int)(orow / a.Hq), head = (int)(orow % a.Hq), D = (int)a.cache.D;
-    int lo = 0, n = (int)a.B;
-    while (n > 1) {                                          // the last request with cu <= t
-        const int step = (n + 63) / 64;
-        const unsigned long long mask = __ballot(lane * step < n && a.cu[lo + lane * step] <= t);
-        const int last = mask ? 63 - __builtin_clzll(mask) : 0;
-        n = min(step, n - last * step);
-        lo += last * step;
+    const int tid = threadIdx.x % kLanes, group = threadIdx.x / kLanes, lane = threadIdx.x & 63;
+    const int64_t rows = a.tokens * a.Hq, orow = (int64_t)blockIdx.x * kRows + group;
+    const int D = (int)a.cache.D;
+    const int used = orow < rows && orow / a.Hq < a.cu[a.B] ? min(p.used[orow], p.splits) : 0;   // (tokens of no request have none)
+    if (used <= 1 && kLanes > 64) return;                    // (all of a workgroup; otherwise it has a barrier to reach)
+    const float *ml = p.part_ml + 2 * orow;
+    // maximum and sum (every wavefront of the row by itself), and the parts' weights
+    float top = -INFINITY, sum = 0.f;
+    for (int s = lane; s < used; s += 64) top = fmaxf(top, ml[2 * s * rows]);
+#pragma unroll
+    for (int sh = 32; sh >= 1; sh >>= 1) top = fmaxf(top, __shfl_xor(top, sh));
+    for (int s = lane; s < used; s += 64) {
+        const float m = ml[2 * s * rows], w = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+        sum += w == 0.f ? 0.f : w * ml[2 * s * rows + 1];
+        w_sh[group][s] = w;                                  // (the same from every wavefront of the row)
     }
-    const Rows rq = rows_of(a, lo);
-    const int R = (t - rq.first) * p.G + head % p.G, row0 = R / kBM * kBM;
-    if (t < rq.first || R >= rq.m * p.G) return;
-    const Span sp = span_of(a, rq, row0 / p.G, (min(row0 + kBM, rq.m * p.G) - 1) / p.G, kStep, p.splits);
-    if (sp.used <= 1) return;
-    float top = -INFINITY;
-    for (int s = 0; s < sp.used; ++s) top = fmaxf(top, p.part_ml[2 * (s * rows + orow)]);
-    float sum = 0.f;
+#pragma unroll
+    for (int sh = 32; sh >= 1; sh >>= 1) sum += __shfl_xor(sum, sh);
+    __syncthreads();
+    const int lanes = D / 4, parts = kLanes / lanes, s0 = tid / lanes, d = 4 * (tid % lanes);
     float4 v{0.f, 0.f, 0.f, 0.f};
-    const int d = 4 * lane;
-    for (int s = 0; s < sp.used; ++s) {
-        const float m = p.part_ml[2 * (s * rows + orow)], w = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
-        if (w == 0.f) continue;
-        sum += w * p.part_ml[2 * (s * rows + orow) + 1];
-        if (d < D) {
-            const float4 e = *reinterpret_cast<const float4 *>(p.part + (s * rows + orow) * D + d);
-            v.x += w * e.x; v.y += w * e.y; v.z += w * e.z; v.w += w * e.w;
+    if (s0 < parts) {
+        const float *src = p.part + orow * D + d;
+#pragma unroll 4
+        for (int s = s0; s < used; s += parts) {
+            const float w = w_sh[group][s];
+            const float4 e = *reinterpret_cast<const float4 *>(src + (int64_t)s * rows * D);
+            if (w != 0.f) { v.x += w * e.x; v.y += w * e.y; v.z += w * e.z; v.w += w * e.w; }
         }
     }
-    const float inv = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;
-    if (d < D)
+    v_sh[group][tid] = v;
+    __syncthreads();
+    if (used > 1 && tid < lanes) {
+        for (int s = 1; s < parts; ++s) {
+            const float4 e = v_sh[group][s * lanes + tid];
+            v.x += e.x; v.y += e.y; v.z += e.z; v.w += e.w;
+        }
+        const float inv = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;
+        const int64_t t = orow / a.Hq, head = orow % a.Hq;
         *reinterpret_cast<u2 *>(static_cast<T *>(a.out) + t * a.out_tok_stride + head * a.out_head_stride + d) =
             u2{pack<T>(v.x * inv, v.y * inv), pack<T>(v.z * inv, v.w * inv)};
-    if (lane == 0 && a.lse) a.lse[orow] = sum != 0.f ? (top + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f : -INFINITY;
+        if (tid == 0 && a.lse) a.lse[orow] = sum != 0.f ? (top + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f : -INFINITY;
+    }
 }
 
 bool misaligned(const void *p, unsigned a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
@@ -464,7 +511,7 @@ int check(const sd_attention &a)
 }
 
 // ---- which kernel, and how many splits: by the shapes alone ----
-struct Plan { int dk, rows, step, tiles, splits; };   // rows of a tile, keys of a step
+struct Plan { int dk, rows, tiles, splits, min_steps; };   // rows of a tile
 Plan plan_of(const sd_attention &a)
 {
     Plan p;
@@ -472,38 +519,42 @@ Plan plan_of(const sd_attention &a)
     p.dk = D <= 64 ? 64 : D <= 96 ? 96 : D <= 128 ? 128 : D <= 192 ? 192 : 256;
     const bool many = rows > 48 * a.B;
     p.rows = many ? 128 : 32;
-    p.step = many ? (p.dk <= 128 ? 64 : 32) : (p.dk <= 128 ? 4 : 2) * 32;
     p.tiles = (int)(rows / p.rows + a.B);
+    const int64_t step = many ? (p.dk <= 128 ? 64 : 32) : (p.dk <= 128 ? 2 : 1) * 32;   // keys
     // enough workgroups for the chip, as far as the longest context allows
     const int64_t there = (rows / p.rows > a.B ? rows / p.rows : a.B) * a.cache.heads;
     int64_t longest = a.width * a.cache.page;
     if (a.window > 0 && a.window + p.rows / G + 1 < longest) longest = a.window + p.rows / G + 1;
-    int64_t splits = there < 512 ? (1024 + there - 1) / there : 1;
-    const int64_t steps = (longest + p.step - 1) / p.step;
-    if (splits > steps) splits = steps;
+    int64_t splits = many ? (there < 256 ? (512 + there - 1) / there : 1) : (2048 + there - 1) / there;
+    p.min_steps = there >= 256 ? 16 : there >= 64 ? 4 : 2;
+    const int64_t most = (longest + p.min_steps * step - 1) / (p.min_steps * step);
+    if (splits > most) splits = most;
     if (splits > 256) splits = 256;
     p.splits = (int)(splits < 1 ? 1 : splits);
     return p;
 }
-size_t part_bytes(const sd_attention &a, const Plan &p) { return p.splits > 1 ? (size_t)p.splits * a.tokens * a.Hq * (a.cache.D + 2) * 4 : 0; }
+// parts, (maximum, sum) of each, and the number of parts of a row
+size_t part_bytes(const sd_attention &a, const Plan &p) { return p.splits > 1 ? (size_t)a.tokens * a.Hq * ((size_t)p.splits * (a.cache.D + 2) + 1) * 4 : 0; }
 
 template <typename T, int DK> void launch(const Attend &p, const Plan &plan, hipStream_t st)
 {
     const dim3 grid((unsigned)(p.a.cache.heads * plan.tiles), (unsigned)plan.splits);
-    const dim3 jgrid((unsigned)((p.a.tokens * p.a.Hq + 3) / 4));
-    constexpr int kPitch = Shape<DK>::kPitch, kKeys = DK <= 128 ? 4 : 2, KT = DK <= 128 ? 64 : 32;
+    constexpr int kPitch = Shape<DK>::kPitch, kKeys = DK <= 128 ? 2 : 1, KT = DK <= 128 ? 64 : 32;
     if (plan.rows == 128) {
         constexpr int bytes = 4 * KT * kPitch;
         hipLaunchKernelGGL((sd_attend_kernel<T, DK, 4, 1, KT>), grid, dim3(256), bytes, st, p);
-        if (plan.splits > 1) hipLaunchKernelGGL((sd_join_kernel<T, 128, KT>), jgrid, dim3(256), 0, st, p);
     } else {
-        constexpr int bytes = kKeys * 4 * 32 * kPitch;
-        static_assert(kKeys * (64 + 32 * (DK + 4)) * 4 <= bytes, "the join has room");
+        constexpr int bytes = kKeys * (4 * 32 * kPitch + 4 * kIds);
+        static_assert(kKeys * (64 + 32 * (DK + 4)) * 4 <= kKeys * 4 * 32 * kPitch, "the join has room");
         static const hipError_t once = hipFuncSetAttribute(reinterpret_cast<const void *>(sd_attend_kernel<T, DK, 1, kKeys, 32>),
                                                            hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
         (void)once;
         hipLaunchKernelGGL((sd_attend_kernel<T, DK, 1, kKeys, 32>), grid, dim3(64 * kKeys), bytes, st, p);
-        if (plan.splits > 1) hipLaunchKernelGGL((sd_join_kernel<T, 32, 32 * kKeys>), jgrid, dim3(256), 0, st, p);
+    }
+    if (plan.splits > 1) {
+        const int64_t rows = p.a.tokens * p.a.Hq;
+        if (plan.splits > 8) hipLaunchKernelGGL((sd_join_kernel<T, 256>), dim3((unsigned)rows), dim3(256), 0, st, p);
+        else hipLaunchKernelGGL((sd_join_kernel<T, 64>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, p);
     }
 }
 template <typename T> void launch(const Attend &p, const Plan &plan, hipStream_t st)
@@ -551,9 +602,11 @@ int sd_attend(const sd_attention *args, void *ws, size_t ws_bytes, void *hip_str
     p.page_mul = (unsigned)((1ull << (31 + s)) / (unsigned long long)a.cache.page + 1);
     p.page_shift = s;
     p.splits = plan.splits;
+    p.min_steps = plan.min_steps;
     p.row_tiles = plan.tiles;
     p.part = static_cast<float *>(ws);
     p.part_ml = p.part + (size_t)plan.splits * a.tokens * a.Hq * a.cache.D;
+    p.used = reinterpret_cast<int *>(p.part_ml + (size_t)plan.splits * a.tokens * a.Hq * 2);
     if (a.cache.dtype == SD_BF16) launch<__bf16>(p, plan, static_cast<hipStream_t>(hip_stream));
     else launch<_Float16>(p, plan, static_cast<hipStream_t>(hip_stream));
     return hipGetLastError() == hipSuccess ? SD_OK : SD_EHIP;

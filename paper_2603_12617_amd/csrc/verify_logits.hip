@@ -1,18 +1,19 @@
 // Verification of drafted tokens from logits (sd_verify_logits): two launches.
 //
-//   stats   every row of V logits in segments of kSeg, a workgroup each: largest logit, its first place, and
-//           sum exp((l - segment's largest) / tau).  All segments are independent, so a batch of one request fills
-//           V / kSeg workgroups a row and a large one the chip; each logit is read once, and stays in registers between
-//           the maximum and the sum.
+//   stats   every row of V logits in segments of kSeg, a workgroup each: the largest logit and, of the rows of requests with a
+//           temperature, sum 2^(l c - top c), c = log2(e) / tau, of greedy ones the largest's first place.  All segments are independent,
+//           so a batch of one request fills V / kSeg workgroups a row and a large one the chip; each logit is read once.
 //   draw    per request and segment: the rows' partial sums are joined (again by every workgroup of the request: a few
-//           hundred numbers from L2, in a fixed order), the drafts tested, and the segment of row n raced:
-//           score(x) = weight(x) / noise(x).  Workgroups of a request meet in a 64-bit maximum of
+//           hundred numbers from L2, in a fixed order, half a wavefront to a row), the drafts tested, and the segment of row n
+//           raced: score(x) = weight(x) / noise(x).  Workgroups of a request meet in a 64-bit maximum of
 //           (score's bits, lowest place), whose order does not matter; the last one writes n and next.
 //
-// Bound by the logits' way from HBM: 2 k + 1 rows a request in `stats`, two rows and the noise again in `draw`.
+// Bound by the logits' way from HBM: 2 k + 1 rows a request in `stats`, two rows and the noise again in `draw`; beside it `stats` has
+// 32 clocks of vector instructions a logit and SIMD lane group (half of them the power of two).
 //
-// exp((l - m) / tau) = 2^((l - m) log2e / tau): the factor is kept as a sum of two floats, since its own rounding would move all
-// of a row's weights together, by |l - m| / tau 6e-8.
+// c is kept as a sum of two floats: its own rounding would move all weights of a row together, by |l - top| c 6e-8.  The low part is
+// positive, so that l = -inf gives a weight of 0 without a test.  What these few instructions cannot do (NaN, +inf, products beyond
+// the float range) shows in a workgroup's maximum and sum, and is done again one by one.
 #include "../../include/specdec.h"
 
 #include <hip/hip_runtime.h>
@@ -20,97 +21,85 @@
 namespace {
 
 typedef unsigned long long u64;
-typedef unsigned int u4 __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kPer = 32;                       // logits of a thread
 constexpr int kSeg = kThreads * kPer;          // of a workgroup
+constexpr int kMaxSegs = (SD_MAX_V + kSeg - 1) / kSeg;
 constexpr float kNone = -__builtin_inff();
+static_assert(kMaxSegs <= 32, "half a wavefront joins a row");
 
-struct Stat { float top, sum; int at; };       // of a row's segment; sum is of exp((l - top) / tau)
-struct Race { u64 residual, target; unsigned met, pad; };   // of a request, cleared by `stats`
+struct Stat { float top, sum; int at; };       // of a row's segment
+struct Race { u64 best; unsigned met, pad; };  // of a request, cleared by `stats`
 
-// ---- element types ----
-template <typename T> struct Vec;              // kVec logits of 16 bytes
+// ---- element types: 16 bytes of logits, at any alignment that the type has ----
+struct bf16 { uint16_t u; };
+typedef float f4u __attribute__((ext_vector_type(4), aligned(4)));
+typedef unsigned u4h __attribute__((ext_vector_type(4), aligned(2)));
+typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ float one(const float *p) { return *p; }
+__device__ __forceinline__ float one(const bf16 *p) { return __uint_as_float((unsigned)p->u << 16); }
+__device__ __forceinline__ float one(const _Float16 *p) { return (float)*p; }
+template <typename T> struct Vec;
 template <> struct Vec<float> {
     static constexpr int kVec = 4;
-    static __device__ __forceinline__ void get(u4 v, float (&f)[4]) { for (int e = 0; e < 4; ++e) f[e] = __uint_as_float(v[e]); }
-    static __device__ __forceinline__ float one(const float *p) { return *p; }
+    typedef f4u Raw;
+    static __device__ __forceinline__ float get(const Raw &v, int e) { return v[e]; }
+    static __device__ __forceinline__ Raw none() { return Raw{kNone, kNone, kNone, kNone}; }
 };
-struct bf16 { uint16_t u; };
 template <> struct Vec<bf16> {
     static constexpr int kVec = 8;
-    static __device__ __forceinline__ void get(u4 v, float (&f)[8])
-    {
-        for (int e = 0; e < 4; ++e) { f[2 * e] = __uint_as_float(v[e] << 16); f[2 * e + 1] = __uint_as_float(v[e] & 0xffff0000u); }
-    }
-    static __device__ __forceinline__ float one(const bf16 *p) { return __uint_as_float((unsigned)p->u << 16); }
+    typedef u4h Raw;
+    static __device__ __forceinline__ float get(const Raw &v, int e) { return __uint_as_float(e & 1 ? v[e / 2] & 0xffff0000u : v[e / 2] << 16); }
+    static __device__ __forceinline__ Raw none() { return Raw{0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u}; }
 };
 template <> struct Vec<_Float16> {
     static constexpr int kVec = 8;
-    static __device__ __forceinline__ void get(u4 v, float (&f)[8])
-    {
-        typedef _Float16 h2 __attribute__((ext_vector_type(2)));
-        for (int e = 0; e < 4; ++e) { const h2 h = __builtin_bit_cast(h2, (unsigned)v[e]); f[2 * e] = (float)h[0]; f[2 * e + 1] = (float)h[1]; }
-    }
-    static __device__ __forceinline__ float one(const _Float16 *p) { return (float)*p; }
+    typedef u4h Raw;
+    static __device__ __forceinline__ float get(const Raw &v, int e) { return (float)__builtin_bit_cast(h2, (unsigned)v[e / 2])[e & 1]; }
+    static __device__ __forceinline__ Raw none() { return Raw{0xfc00fc00u, 0xfc00fc00u, 0xfc00fc00u, 0xfc00fc00u}; }
 };
+// kVec logits from place x of a row of V; those past its end are -inf
+template <typename T> __device__ __forceinline__ typename Vec<T>::Raw load(const T *row, int x, int V)
+{
+    typedef Vec<T> E;
+    if (x + E::kVec <= V) return *reinterpret_cast<const typename E::Raw *>(row + x);
+    typename E::Raw v = E::none();
+    for (int e = 0; e < E::kVec; ++e)
+        if (x + e < V) {
+            if (sizeof(T) == 4) v[e] = __builtin_bit_cast(decltype(v[0] + v[0]), *reinterpret_cast<const unsigned *>(row + x + e));
+            else {
+                const unsigned h = *reinterpret_cast<const uint16_t *>(row + x + e), old = __builtin_bit_cast(unsigned, v[e / 2]);
+                v[e / 2] = __builtin_bit_cast(decltype(v[0] + v[0]), e & 1 ? (old & 0xffffu) | h << 16 : (old & 0xffff0000u) | h);
+            }
+        }
+    return v;
+}
+// a thread's logits of segment `seg`: raw[c] from place place(seg, c) on
+template <typename T> __device__ __forceinline__ int place(int seg, int c) { return seg * kSeg + (c * kThreads + (int)threadIdx.x) * Vec<T>::kVec; }
 
 // NaN counts as -inf, +inf as the largest float
-__device__ __forceinline__ float logit(float l) { return l == l ? fminf(l, 3.4028234663852886e38f) : kNone; }
+__device__ __forceinline__ float clean(float l) { return l == l ? fminf(l, 3.4028234663852886e38f) : kNone; }
 
-// the logits of a thread's share of segment `seg`: places seg * kSeg + (c * kThreads + tid) * kVec + e
-template <typename T, bool WIDE>
-__device__ __forceinline__ void load_row(const T *row, int seg, int V, float (&f)[kPer])
-{
-    constexpr int kVec = Vec<T>::kVec;
-    if (WIDE) {
-        u4 v[kPer / kVec];
-#pragma unroll
-        for (int c = 0; c < kPer / kVec; ++c) {
-            const int x = seg * kSeg + (c * kThreads + (int)threadIdx.x) * kVec;
-            if (x < V) v[c] = *reinterpret_cast<const u4 *>(row + x);
-        }
-#pragma unroll
-        for (int c = 0; c < kPer / kVec; ++c) {
-            const int x = seg * kSeg + (c * kThreads + (int)threadIdx.x) * kVec;
-            float g[kVec];
-            Vec<T>::get(v[c], g);
-#pragma unroll
-            for (int e = 0; e < kVec; ++e) f[c * kVec + e] = x < V ? logit(g[e]) : kNone;
-        }
-    } else {
-#pragma unroll
-        for (int c = 0; c < kPer / kVec; ++c)
-#pragma unroll
-            for (int e = 0; e < kVec; ++e) {
-                const int x = seg * kSeg + (c * kVec + e) * kThreads + (int)threadIdx.x;
-                f[c * kVec + e] = x < V ? logit(Vec<T>::one(row + x)) : kNone;
-            }
-    }
-}
-// the place of f[i] above
-template <typename T, bool WIDE> __device__ __forceinline__ int place(int seg, int i)
-{
-    constexpr int kVec = Vec<T>::kVec;
-    return WIDE ? seg * kSeg + ((i / kVec) * kThreads + (int)threadIdx.x) * kVec + i % kVec : seg * kSeg + i * kThreads + (int)threadIdx.x;
-}
-
-// ---- temperature: exp((l - top) / tau) ----
-struct Heat { float hi, lo; };                 // log2(e) / tau as a sum
+// ---- temperature ----
+struct Heat { float hi, lo; };                 // log2(e) / tau as a sum, lo > 0
 __device__ __forceinline__ Heat heat(float tau)
 {
-    const double c = fmin(1.4426950408889634 / (double)tau, 1e30);
+    const double c = fmax(fmin(1.4426950408889634 / (double)tau, 1e30), 1e-30);
     Heat h;
     h.hi = (float)c;
-    h.lo = (float)(c - (double)h.hi);
+    if ((double)h.hi > c) h.hi = __uint_as_float(__float_as_uint(h.hi) - 1);
+    h.lo = fmaxf((float)(c - (double)h.hi), 1e-37f);
     return h;
 }
-// (below 2^-125 of the largest: 0, as for l = -inf and where l - top is no number)
-__device__ __forceinline__ float weight(float l, float top, Heat h)
+// whether l c - top c stays in the float range for every l <= top
+__device__ __forceinline__ bool tame(float top, Heat h) { return fabsf(top * h.hi) < 1e30f; }
+__device__ __forceinline__ float power(float l, float ref, Heat h) { return __builtin_amdgcn_exp2f(__builtin_fmaf(l, h.lo, __builtin_fmaf(l, h.hi, -ref))); }
+// the same of any clean logit (below 2^-125 of the largest: 0)
+__device__ __forceinline__ float power_any(float l, float top, Heat h)
 {
     const float d = l - top;
-    return d * h.hi >= -125.f ? __builtin_amdgcn_exp2f(__builtin_fmaf(d, h.hi, d * h.lo)) : 0.f;
+    return d * h.hi >= -125.f ? __builtin_amdgcn_exp2f(__builtin_fmaf(d, h.lo, d * h.hi)) : 0.f;
 }
 
 // the request of a row: the last b with cu[b] <= row (target rows) or cu[b] - b <= row (drafts' rows); by the lanes of a wavefront
@@ -128,37 +117,64 @@ __device__ __forceinline__ int request_of(const int32_t *cu, int B, int row, boo
     return lo;
 }
 
-template <typename T, bool WIDE>
+template <typename T>
 __global__ void __launch_bounds__(kThreads) sd_stats_kernel(const sd_logits s, Stat *stat, Race *race)
 {
+    typedef Vec<T> E;
+    constexpr int kC = kPer / E::kVec;
     __shared__ float top_sh[kWaves], sum_sh[kWaves];
     __shared__ int at_sh[kWaves];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int B = (int)s.B, V = (int)s.V, rows = (int)s.rows;
     const int row = blockIdx.x, seg = blockIdx.y;
-    if (seg == 0 && row < B && tid == 0) race[row] = Race{0, 0, 0, 0};
+    if (seg == 0 && row < B && tid == 0) race[row] = Race{0, 0, 0};
     const bool draft = row >= rows;
     const T *l = draft ? static_cast<const T *>(s.q) + (int64_t)(row - rows) * s.q_stride : static_cast<const T *>(s.p) + (int64_t)row * s.p_stride;
-    float f[kPer];
-    load_row<T, WIDE>(l, seg, V, f);
-    const float tau = s.tau[request_of(s.cu, B, draft ? row - rows : row, draft, lane)];
-    float top = kNone;
+    typename E::Raw raw[kC];
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) top = fmaxf(top, f[i]);
+    for (int c = 0; c < kC; ++c) raw[c] = load(l, place<T>(seg, c), V);
+    const float tau = s.tau[request_of(s.cu, B, draft ? row - rows : row, draft, lane)];
+    const bool hot = tau > 0.f;
+    const Heat h = heat(hot ? tau : 1.f);
+    float top = kNone;                         // (a maximum leaves NaN out)
+#pragma unroll
+    for (int c = 0; c < kC; ++c)
+#pragma unroll
+        for (int e = 0; e < E::kVec; ++e) top = fmaxf(top, E::get(raw[c], e));
 #pragma unroll
     for (int sh = 32; sh >= 1; sh >>= 1) top = fmaxf(top, __shfl_xor(top, sh));
     if (lane == 0) top_sh[wave] = top;
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) top = fmaxf(top, top_sh[w]);
-    const bool hot = tau > 0.f;
-    const Heat h = heat(hot ? tau : 1.f);
     int at = 0x7fffffff;
     float sum = 0.f;
+    if (hot) {
+        const float ref = top * h.hi;
+        bool odd = !tame(top, h);
+        if (!odd) {
 #pragma unroll
-    for (int i = kPer - 1; i >= 0; --i) {
-        if (f[i] == top) at = min(at, place<T, WIDE>(seg, i));
-        sum += weight(f[i], top, h);
+            for (int c = 0; c < kC; ++c)
+#pragma unroll
+                for (int e = 0; e < E::kVec; ++e) sum += power(E::get(raw[c], e), ref, h);
+            odd = sum != sum;
+        }
+        if (odd) {
+            sum = 0.f;
+#pragma unroll
+            for (int c = 0; c < kC; ++c)
+#pragma unroll
+                for (int e = 0; e < E::kVec; ++e) {
+                    const float v = clean(E::get(raw[c], e));
+                    sum += tame(top, h) ? power(v, ref, h) : power_any(v, clean(top), h);
+                }
+        }
+    } else {
+#pragma unroll
+        for (int c = kC - 1; c >= 0; --c)
+#pragma unroll
+            for (int e = E::kVec - 1; e >= 0; --e)
+                if (E::get(raw[c], e) == top) at = place<T>(seg, c) + e;
     }
 #pragma unroll
     for (int sh = 32; sh >= 1; sh >>= 1) { at = min(at, __shfl_xor(at, sh)); sum += __shfl_xor(sum, sh); }
@@ -166,139 +182,191 @@ __global__ void __launch_bounds__(kThreads) sd_stats_kernel(const sd_logits s, S
     __syncthreads();
     if (tid == 0) {
         Stat r;
-        r.top = top;
+        r.top = clean(top);
         r.sum = (sum_sh[0] + sum_sh[1]) + (sum_sh[2] + sum_sh[3]);
         r.at = min(min(at_sh[0], at_sh[1]), min(at_sh[2], at_sh[3]));
         stat[(int64_t)row * gridDim.y + seg] = r;
     }
 }
 
-// a row's parts joined by the lanes of a wavefront, in a fixed order; every lane gets the result
-struct Row { float top; float inv; int best; };   // inv: 1 / sum exp((l - top) / tau), 0 without a finite logit
+// A row's parts joined by the 32 lanes of half a wavefront, in a fixed order; each of them gets the result.
+struct Row { float top, inv; int best; };      // inv: 1 / the sum of the weights, 0 without a finite logit
 __device__ __forceinline__ Row join(const Stat *stat, int segs, Heat h, int lane)
 {
-    float top = kNone;
-    int best = 0x7fffffff;
-    for (int s = lane; s < segs; s += 64) top = fmaxf(top, stat[s].top);
+    const int s = lane & 31;
+    Stat r{kNone, 0.f, 0x7fffffff};
+    if (s < segs) r = stat[s];
+    float top = r.top;
 #pragma unroll
-    for (int sh = 32; sh >= 1; sh >>= 1) top = fmaxf(top, __shfl_xor(top, sh));
+    for (int sh = 16; sh >= 1; sh >>= 1) top = fmaxf(top, __shfl_xor(top, sh));
+    int best = r.top == top ? r.at : 0x7fffffff;
+    // (sums are relative to top c rounded to float where that is tame)
     double sum = 0.0;
-    for (int s = lane; s < segs; s += 64) {
-        const Stat r = stat[s];
-        if (r.top == top) best = min(best, r.at);
-        if (r.top > kNone) sum += (double)r.sum * (double)weight(r.top, top, h);
+    if (r.top > kNone) {
+        const float back = tame(top, h) && tame(r.top, h) ? exp2f((float)((double)(r.top * h.hi) - (double)(top * h.hi))) : power_any(r.top, top, h);
+        sum = (double)r.sum * (double)back;
     }
 #pragma unroll
-    for (int sh = 32; sh >= 1; sh >>= 1) { best = min(best, __shfl_xor(best, sh)); sum += __shfl_xor(sum, sh); }
-    Row r;
-    r.top = top;
-    r.best = best;
-    r.inv = top > kNone ? (float)(1.0 / sum) : 0.f;
-    return r;
+    for (int sh = 16; sh >= 1; sh >>= 1) { best = min(best, __shfl_xor(best, sh)); sum += __shfl_xor(sum, sh); }
+    Row w;
+    w.top = top;
+    w.best = top > kNone ? best : 0;
+    w.inv = top > kNone ? (float)(1.0 / sum) : 0.f;
+    return w;
+}
+
+// a probability
+__device__ __forceinline__ float weight(float l, const Row &r, Heat h)
+{
+    return (tame(r.top, h) && l == l ? power(l, r.top * h.hi, h) : power_any(clean(l), r.top, h)) * r.inv;
 }
 
 // larger scores win, of equal ones the lowest place
 __device__ __forceinline__ u64 entry(float score, int x) { return ((u64)__float_as_uint(score) << 32) | (0xffffffffu - (unsigned)x); }
+__device__ __forceinline__ u64 larger(u64 a, u64 b) { return a > b ? a : b; }
 
-template <typename T, bool WIDE>
+// the largest entry of a workgroup, for thread 0
+__device__ __forceinline__ u64 first_of(u64 v, u64 *sh)
+{
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) v = larger(v, __shfl_xor(v, d));
+    if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
+    __syncthreads();
+    return larger(larger(sh[0], sh[1]), larger(sh[2], sh[3]));
+}
+
+template <typename T>
 __global__ void __launch_bounds__(kThreads) sd_draw_kernel(const sd_logits s, const Stat *stat, Race *race, int segs, int32_t *n_out, int32_t *next_out)
 {
-    __shared__ int n_sh;
-    __shared__ u64 best_sh[2][kWaves];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    typedef Vec<T> E;
+    constexpr int kC = kPer / E::kVec;
+    constexpr int kKeep = SD_MAX_K + 1;                     // rows whose parts are kept joined; further ones are joined again
+    __shared__ Row row_sh[2][kKeep];
+    __shared__ int n_sh, last_sh;
+    __shared__ u64 best_sh[kWaves];
+    const int tid = threadIdx.x, lane = tid & 63;
     const int V = (int)s.V, rows = (int)s.rows, drafts = rows - (int)s.B;
     const int b = blockIdx.x, seg = blockIdx.y;
     const int row0 = min(max(s.cu[b], 0), rows - 1), row1 = min(max(s.cu[b + 1], row0 + 1), rows);
-    const int k = row1 - row0 - 1, first = min(max(row0 - b, 0), drafts);   // drafts first .. first + k - 1
+    const int first = min(max(row0 - b, 0), drafts), k = min(row1 - row0 - 1, drafts - first);   // drafts first .. first + k - 1
     const float tau = s.tau[b];
     const bool hot = tau > 0.f;
     const Heat h = heat(hot ? tau : 1.f);
     const T *P = static_cast<const T *>(s.p), *Q = static_cast<const T *>(s.q);
+    const float *noise = s.noise + (int64_t)b * s.noise_stride;
+    typename Vec<float>::Raw e[kC * E::kVec / 4];
+    if (hot) {                                              // (under way while the drafts are tested)
+#pragma unroll
+        for (int c = 0; c < kC; ++c)
+#pragma unroll
+            for (int i = 0; i < E::kVec / 4; ++i) e[c * (E::kVec / 4) + i] = load(noise, place<T>(seg, c) + 4 * i, V);
+    }
     if (tid == 0) n_sh = k;
     __syncthreads();
-    for (int j = wave; j < k && first + j < drafts; j += kWaves) {
-        const int x = min(max(s.tok[first + j], 0), V - 1);
-        const Row p = join(stat + (int64_t)(row0 + j) * segs, segs, h, lane);
-        bool ok;
-        if (hot) {
-            const float px = weight(logit(Vec<T>::one(P + (int64_t)(row0 + j) * s.p_stride + x)), p.top, h) * p.inv;
-            float qx = 1.f;
-            if (Q) {
-                const Row q = join(stat + (int64_t)(rows + first + j) * segs, segs, h, lane);
-                qx = weight(logit(Vec<T>::one(Q + (int64_t)(first + j) * s.q_stride + x)), q.top, h) * q.inv;
+    // half a wavefront to a draft: its target row and, if there is one, its own
+    for (int j0 = 0; j0 <= k; j0 += kThreads / 32) {
+        const int j = j0 + tid / 32;
+        if (j <= k) {
+            int x = 0;
+            float pl = 0.f, ql = 0.f, r = 0.f;
+            if (j < k) {
+                x = min(max(s.tok[first + j], 0), V - 1);
+                if (hot) {
+                    r = s.r[first + j];
+                    pl = one(P + (int64_t)(row0 + j) * s.p_stride + x);
+                    if (Q) ql = one(Q + (int64_t)(first + j) * s.q_stride + x);
+                }
             }
-            ok = __fmul_rn(s.r[first + j], qx) <= px;
-        } else {
-            ok = x == p.best;
+            const Row p = join(stat + (int64_t)(row0 + j) * segs, segs, h, lane);
+            Row q{0.f, 0.f, 0};
+            if (Q && j < k) q = join(stat + (int64_t)(rows + first + j) * segs, segs, h, lane);
+            if ((tid & 31) == 0) {
+                if (j < kKeep) { row_sh[0][j] = p; row_sh[1][j] = q; }
+                if (j < k && !(hot ? __fmul_rn(r, Q ? weight(ql, q, h) : 1.f) <= weight(pl, p, h) : x == p.best)) atomicMin(&n_sh, j);
+            }
         }
-        if (!ok) { if (lane == 0) atomicMin(&n_sh, j); break; }
+        __syncthreads();
+        if (n_sh < j0 + kThreads / 32) break;               // (the same for everyone: nobody writes before all have read)
+        __syncthreads();
     }
-    __syncthreads();
     const int n = n_sh;
-    const Row p = join(stat + (int64_t)(row0 + n) * segs, segs, h, lane);
+    const bool rejected = n < k;
+    Row p, q{0.f, 0.f, 0};
+    if (n < kKeep) { p = row_sh[0][n]; q = row_sh[1][n]; }
+    else {
+        p = join(stat + (int64_t)(row0 + n) * segs, segs, h, lane);
+        if (Q && rejected) q = join(stat + (int64_t)(rows + first + n) * segs, segs, h, lane);
+    }
     if (!hot || p.top == kNone) {
         if (seg == 0 && tid == 0) { n_out[b] = n; next_out[b] = p.top == kNone ? 0 : p.best; }
         return;
     }
-    const bool rejected = n < k && first + n < drafts;
-    float f[kPer], g[kPer], e[kPer];
-    load_row<T, WIDE>(P + (int64_t)(row0 + n) * s.p_stride, seg, V, f);
-    const float *noise = s.noise + (int64_t)b * s.noise_stride;
+    const T *prow = P + (int64_t)(row0 + n) * s.p_stride, *qrow = Q && rejected ? Q + (int64_t)(first + n) * s.q_stride : nullptr;
+    typename E::Raw f[kC], g[kC];
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-        const int x = place<T, WIDE>(seg, i);
-        e[i] = x < V ? noise[x] : 1.f;
+    for (int c = 0; c < kC; ++c) f[c] = load(prow, place<T>(seg, c), V);
+    if (qrow) {
+#pragma unroll
+        for (int c = 0; c < kC; ++c) g[c] = load(qrow, place<T>(seg, c), V);
+    } else {
+#pragma unroll
+        for (int c = 0; c < kC; ++c) g[c] = E::none();
     }
-    Row q{0.f, 0.f, 0};
-    int drafted = -1;
-    if (rejected) {
-        if (Q) {
-            q = join(stat + (int64_t)(rows + first + n) * segs, segs, h, lane);
-            load_row<T, WIDE>(Q + (int64_t)(first + n) * s.q_stride, seg, V, g);
-        } else {
-            drafted = min(max(s.tok[first + n], 0), V - 1);
+    const int drafted = rejected && !Q ? min(max(s.tok[first + n], 0), V - 1) : -1;
+    float won = 0.f;
+    int at = 0;
+    if (tame(p.top, h) && tame(q.top, h)) {
+        const float pref = p.top * h.hi, qref = q.top * h.hi;
+#pragma unroll
+        for (int c = 0; c < kC; ++c)
+#pragma unroll
+            for (int i = 0; i < E::kVec; ++i) {
+                float w = power(E::get(f[c], i), pref, h) * p.inv;
+                // (the maximum takes what is no number for 0; q.inv = 0 without a rejected draft's row)
+                if (qrow) w = __builtin_fmaf(fmaxf(power(E::get(g[c], i), qref, h), 0.f), -q.inv, w);
+                else if (drafted == place<T>(seg, c) + i) w = 0.f;
+                const float sc = w * __builtin_amdgcn_rcpf(e[(c * E::kVec + i) / 4][i % 4]);
+                if (sc > won) { won = sc; at = c * E::kVec + i; }     // (places ascend within a thread: of equal scores the first stays)
+            }
+    } else {
+#pragma unroll
+        for (int c = 0; c < kC; ++c)
+#pragma unroll
+            for (int i = 0; i < E::kVec; ++i) {
+                float w = weight(E::get(f[c], i), p, h);
+                if (qrow) w -= weight(E::get(g[c], i), q, h);
+                else if (drafted == place<T>(seg, c) + i) w = 0.f;
+                const float sc = w * __builtin_amdgcn_rcpf(e[(c * E::kVec + i) / 4][i % 4]);
+                if (sc > won) { won = sc; at = c * E::kVec + i; }
+            }
+    }
+    u64 best = first_of(won > 0.f ? entry(won, place<T>(seg, at / E::kVec) + at % E::kVec) : 0, best_sh);
+    if (tid == 0) {
+        bool last = true;
+        if (segs > 1) {
+            // Only atomics carry data between the workgroups, each done (its old value is back) before the next is issued: a fence,
+            // which would write back and drop caches, is not needed for that.
+            if (best) {
+                u64 old = __hip_atomic_fetch_max(&race[b].best, best, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                asm volatile("s_waitcnt vmcnt(0)" : "+v"(old)::"memory");
+            }
+            last = __hip_atomic_fetch_add(&race[b].met, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (unsigned)segs - 1;
+            if (last) best = __hip_atomic_fetch_max(&race[b].best, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         }
-    }
-    // the races for the residual and for the target (which counts where the residual is zero everywhere)
-    float won[2] = {0.f, 0.f};
-    int at[2] = {0x7fffffff, 0x7fffffff};
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-        const int x = place<T, WIDE>(seg, i);
-        const float w = weight(f[i], p.top, h) * p.inv;
-        float left = w;
-        if (rejected) left = Q ? w - weight(g[i], q.top, h) * q.inv : x == drafted ? 0.f : w;
-        // (places of a thread ascend, so of equal scores the first stays)
-        if (left > 0.f) { const float sc = left / e[i]; if (sc > won[0]) { won[0] = sc; at[0] = x; } }
-        if (rejected && w > 0.f) { const float sc = w / e[i]; if (sc > won[1]) { won[1] = sc; at[1] = x; } }
-    }
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {
-        u64 v = won[c] > 0.f ? entry(won[c], at[c]) : 0;
-#pragma unroll
-        for (int sh = 32; sh >= 1; sh >>= 1) { const u64 o = __shfl_xor(v, sh); v = o > v ? o : v; }
-        if (lane == 0) best_sh[c][wave] = v;
+        if (last && (best || !rejected)) { n_out[b] = n; next_out[b] = best ? (int)(0xffffffffu - (unsigned)best) : 0; }
+        last_sh = last && !best && rejected;
     }
     __syncthreads();
-    if (tid == 0) {
-        u64 v[2] = {0, 0};
-#pragma unroll
-        for (int c = 0; c < 2; ++c)
-            for (int w = 0; w < kWaves; ++w) v[c] = best_sh[c][w] > v[c] ? best_sh[c][w] : v[c];
-        if (segs > 1) {
-            // only atomics carry data between the workgroups, so their order is all that is needed
-            if (v[0]) atomicMax(&race[b].residual, v[0]);
-            if (v[1]) atomicMax(&race[b].target, v[1]);
-            __threadfence();
-            if (atomicAdd(&race[b].met, 1u) != (unsigned)segs - 1) return;
-            __threadfence();
-            v[0] = atomicMax(&race[b].residual, 0ull);
-            v[1] = atomicMax(&race[b].target, 0ull);
-        }
-        const u64 best = v[0] ? v[0] : v[1];
-        n_out[b] = n;
-        next_out[b] = best ? (int)(0xffffffffu - (unsigned)best) : 0;
+    if (!last_sh) return;
+    // The residual is zero everywhere: the last workgroup races the target's whole row.
+    won = 0.f;
+    int x_won = 0;
+    for (int x = tid; x < V; x += kThreads) {
+        const float sc = weight(one(prow + x), p, h) * __builtin_amdgcn_rcpf(noise[x]);
+        if (sc > won) { won = sc; x_won = x; }
     }
+    best = first_of(won > 0.f ? entry(won, x_won) : 0, best_sh);
+    if (tid == 0) { n_out[b] = n; next_out[b] = best ? (int)(0xffffffffu - (unsigned)best) : 0; }
 }
 
 bool misaligned(const void *p, unsigned a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
@@ -315,11 +383,11 @@ int segments(const sd_logits &s) { return (int)((s.V + kSeg - 1) / kSeg); }
 int64_t stat_rows(const sd_logits &s) { return s.rows + (s.q ? s.rows - s.B : 0); }
 size_t race_bytes(const sd_logits &s) { return (size_t)s.B * sizeof(Race); }
 
-template <typename T, bool WIDE> void launch(const sd_logits &s, Stat *stat, Race *race, int32_t *n, int32_t *next, hipStream_t st)
+template <typename T> void launch(const sd_logits &s, Stat *stat, Race *race, int32_t *n, int32_t *next, hipStream_t st)
 {
     const unsigned segs = (unsigned)segments(s);
-    hipLaunchKernelGGL((sd_stats_kernel<T, WIDE>), dim3((unsigned)stat_rows(s), segs), dim3(kThreads), 0, st, s, stat, race);
-    hipLaunchKernelGGL((sd_draw_kernel<T, WIDE>), dim3((unsigned)s.B, segs), dim3(kThreads), 0, st, s, stat, race, (int)segs, n, next);
+    hipLaunchKernelGGL(sd_stats_kernel<T>, dim3((unsigned)stat_rows(s), segs), dim3(kThreads), 0, st, s, stat, race);
+    hipLaunchKernelGGL(sd_draw_kernel<T>, dim3((unsigned)s.B, segs), dim3(kThreads), 0, st, s, stat, race, (int)segs, n, next);
 }
 
 }  // namespace
@@ -348,12 +416,9 @@ int sd_verify_logits(const sd_logits *a, int32_t *n_dev, int32_t *next_dev, void
     Race *race = static_cast<Race *>(ws);
     Stat *stat = reinterpret_cast<Stat *>(static_cast<char *>(ws) + race_bytes(s));
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    // 16-byte loads need rows that start and end on 16 bytes
-    const unsigned vec = 16 / es;
-    const bool wide = s.V % vec == 0 && s.p_stride % vec == 0 && !misaligned(s.p, 16) && (!s.q || (s.q_stride % vec == 0 && !misaligned(s.q, 16)));
-    if (s.dtype == SD_F32) { if (wide) launch<float, true>(s, stat, race, n_dev, next_dev, st); else launch<float, false>(s, stat, race, n_dev, next_dev, st); }
-    else if (s.dtype == SD_BF16) { if (wide) launch<bf16, true>(s, stat, race, n_dev, next_dev, st); else launch<bf16, false>(s, stat, race, n_dev, next_dev, st); }
-    else { if (wide) launch<_Float16, true>(s, stat, race, n_dev, next_dev, st); else launch<_Float16, false>(s, stat, race, n_dev, next_dev, st); }
+    if (s.dtype == SD_F32) launch<float>(s, stat, race, n_dev, next_dev, st);
+    else if (s.dtype == SD_BF16) launch<bf16>(s, stat, race, n_dev, next_dev, st);
+    else launch<_Float16>(s, stat, race, n_dev, next_dev, st);
     return hipGetLastError() == hipSuccess ? SD_OK : SD_EHIP;
 }
 
