@@ -27,6 +27,8 @@
 
 #include <math.h>
 
+#include <type_traits>
+
 namespace {
 
 typedef unsigned int u2 __attribute__((ext_vector_type(2)));
@@ -60,6 +62,27 @@ __device__ __forceinline__ f2 halves(float x)
 {
     const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     return f2{__uint_as_float(r[0]), __uint_as_float(r[1])};
+}
+
+// f(0), f(1), .. f(N - 1), each with its number as a type
+template <int N, int I = 0, typename F> __device__ __forceinline__ void unroll(F f)
+{
+    if constexpr (I < N) {
+        f(std::integral_constant<int, I>());
+        unroll<N, I + 1>(f);
+    }
+}
+// an address from lane I of each 16 lanes (kSides = 2: from lane 2 I for the first eight of them, lane 2 I + 1 for the others)
+template <int I, int kSides> __device__ __forceinline__ int from_lane(int x)
+{
+    if constexpr (kSides == 1) return __builtin_amdgcn_update_dpp(0, x, 0x150 + I, 0xF, 0xF, false);                 // row_newbcast
+    else return __builtin_amdgcn_update_dpp(__builtin_amdgcn_update_dpp(0, x, 0x150 + 2 * I, 0xF, 0xF, false), x, 0x150 + 2 * I + 1, 0xF, 0xC, false);
+}
+template <int I, int kSides> __device__ __forceinline__ const char *from_lane(const char *x)
+{
+    const uint64_t u = reinterpret_cast<uint64_t>(x);
+    const uint64_t lo = (unsigned)from_lane<I, kSides>((int)(unsigned)u), hi = (unsigned)from_lane<I, kSides>((int)(unsigned)(u >> 32));
+    return reinterpret_cast<const char *>(hi << 32 | lo);
 }
 
 struct Attend {
@@ -144,7 +167,7 @@ template <int DK> struct Shape {
     static __device__ __forceinline__ int v_at(int row, int c) { return kPieces >= 16 ? c ^ (4 * (row & 3)) : c ^ (4 * ((row >> 1) & 1)); }
 };
 
-template <typename T, int DK, int kRows, int kKeys, int KT>
+template <typename T, int DK, bool kFull, int kRows, int kKeys, int KT>
 __global__ void __launch_bounds__(64 * kRows * kKeys, kRows == 1 && DK > 128 ? 1 : 2) sd_attend_kernel(const Attend p)
 {
     static_assert(kRows == 1 || kKeys == 1, "wavefronts differ in rows or in keys");
@@ -154,13 +177,20 @@ __global__ void __launch_bounds__(64 * kRows * kKeys, kRows == 1 && DK > 128 ? 1
     constexpr int kLoads = KT / S::kPerLoad / kRows;         // of a wavefront, per tile and side
     constexpr int kBlocks = KT / 32, kD = DK / 32, kQ = DK / 16;
     constexpr int kBM = 32 * kRows;
+    constexpr int kSides = S::kPieces >= 16 ? 1 : 2;         // rows of a load within 16 lanes
+    static_assert(kLoads * kSides <= 16, "16 lanes hold the keys of their loads");
     extern __shared__ char lds[];
     const sd_attention &a = p.a;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = kRows > 1 ? wave : 0, wk = kRows > 1 ? 0 : wave;
     const int half = lane >> 5, col = lane & 31;
-    const int kh = blockIdx.x % (unsigned)a.cache.heads, x = p.row_tiles - 1 - (int)(blockIdx.x / (unsigned)a.cache.heads), split = blockIdx.y;   // (the rows with most keys first)
-    const int D = (int)a.cache.D, G = p.G, page = (int)a.cache.page;
+    // The chip deals workgroups to its eight dies in turn.  Chunks: the tiles of a key head to one die, whose cache then holds its keys, the tiles with
+    // most keys first.  Decoding, where keys are read once: the heads of a range of keys one after the other on one die, so that the pieces of a token's
+    // row are fetched at about the same time.
+    const unsigned heads = (unsigned)a.cache.heads, turn = kOwn ? blockIdx.x / 8 : blockIdx.x, item = kOwn ? turn / heads * 8 + blockIdx.x % 8 : turn / heads;
+    const int kh = turn % heads, split = item / (unsigned)p.row_tiles, x = p.row_tiles - 1 - (int)(item % (unsigned)p.row_tiles);
+    if (split >= p.splits) return;
+    const int D = kFull ? DK : (int)a.cache.D, G = p.G, page = (int)a.cache.page;
 
     const int b = request_of(a.cu, (int)a.B, G, kBM, x, lane);
     const Rows rq = rows_of(a, b);
@@ -183,7 +213,7 @@ __global__ void __launch_bounds__(64 * kRows * kKeys, kRows == 1 && DK > 128 ? 1
     const int any_to = row0 + wm * 32 < rows ? see_to(rq, w1) : 0;
 
     char *const kbuf = lds + wk * 4 * kTile, *const vbuf = kbuf + 2 * kTile;
-    if (D < DK) {                                            // pieces past D are never loaded
+    if (!kFull) {                                            // pieces past D are never loaded
         for (int i = tid; i < kKeys * 4 * kTile / 16; i += 64 * kRows * kKeys) reinterpret_cast<u4 *>(lds)[i] = u4{0, 0, 0, 0};
         __syncthreads();
     }
@@ -199,37 +229,33 @@ __global__ void __launch_bounds__(64 * kRows * kKeys, kRows == 1 && DK > 128 ? 1
     }
 
     // ---- from the pages to LDS: load i of a tile brings rows (i * kRows + wm) * kPerLoad + lane / kPieces ----
+    // Where a key lies is worked out once a tile by one of the 16 lanes that load from it (lane i of 16 for load i; for rows of eight pieces,
+    // lanes 2 i and 2 i + 1), and handed to the others as the load is issued.
     const int lrow = wm * S::kPerLoad + lane / S::kPieces, lpiece = lane % S::kPieces;
+    const int own_row = min((lane & 15) / kSides, kLoads - 1) * kRows * S::kPerLoad + wm * S::kPerLoad +
+                        (kSides == 1 ? lane / S::kPieces : 2 * (lane >> 4) + (lane & 1));
     const char *const kbase = static_cast<const char *>(a.cache.k) + 2 * (int64_t)kh * a.cache.k_head_stride;
     const char *const vbase = static_cast<const char *>(a.cache.v) + 2 * (int64_t)kh * a.cache.v_head_stride;
     const int32_t *const table = a.table + (int64_t)b * a.table_stride;
     // (places that none of the tile's rows sees get a key that one does see, so that a zero weight never meets what a page happens to hold)
     auto key_in = [&](int key) { return min(max(key, first_key), last_key); };
-    auto key_of = [&](int t, int i) { return key_in(t * KT + i * kRows * S::kPerLoad + lrow); };
+    auto own_key = [&](int t) { return key_in(t * KT + own_row); };
     const unsigned kto = __builtin_amdgcn_readfirstlane(lds_address(kbuf)), vto = __builtin_amdgcn_readfirstlane(lds_address(vbuf));
     auto issue = [&](int t, int buf, auto page_id) {
-        const char *ks[kLoads], *vs[kLoads];
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const int key = key_of(t, i), row = i * kRows * S::kPerLoad + lrow, place = page_of(p, key);
-            const int at = key - place * page;
-            const int64_t id = min(max(page_id(i, place), 0), (int)a.cache.pages - 1);
-            ks[i] = kbase + 2 * (id * a.cache.k_page_stride + at * a.cache.k_tok_stride) + 16 * S::k_at(row, lpiece);
-            vs[i] = vbase + 2 * (id * a.cache.v_page_stride + at * a.cache.v_tok_stride) + 16 * S::v_at(row, lpiece);
-        }
+        const int key = own_key(t), place = page_of(p, key), at = key - place * page;
+        const int64_t id = min(max(page_id(place), 0), (int)a.cache.pages - 1);
+        const char *const ks = kbase + 2 * (id * a.cache.k_page_stride + at * a.cache.k_tok_stride);
+        const char *const vs = vbase + 2 * (id * a.cache.v_page_stride + at * a.cache.v_tok_stride);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // what was read from the buffer is there
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const unsigned at = buf * kTile + (i * kRows + wm) * 1024;
-            if (D == DK) {
-                load_to_lds(ks[i], kto + at);
-                load_to_lds(vs[i], vto + at);
-            } else {                                         // (every row has a piece below D, so every load is issued)
-                const int row = i * kRows * S::kPerLoad + lrow;
-                if (8 * S::k_at(row, lpiece) < D) load_to_lds(ks[i], kto + at);
-                if (8 * S::v_at(row, lpiece) < D) load_to_lds(vs[i], vto + at);
-            }
-        }
+        unroll<kLoads>([&](auto n) {
+            constexpr int i = decltype(n)::value;
+            const int row = i * kRows * S::kPerLoad + lrow;
+            const unsigned to = buf * kTile + (i * kRows + wm) * 1024;
+            const int kp = S::k_at(row, lpiece), vp = S::v_at(row, lpiece);
+            const char *const kx = from_lane<i, kSides>(ks) + 16 * kp, *const vx = from_lane<i, kSides>(vs) + 16 * vp;   // (with all lanes on)
+            if (kFull || 8 * kp < D) load_to_lds(kx, kto + to);     // (every row has a piece below D, so every load is issued)
+            if (kFull || 8 * vp < D) load_to_lds(vx, vto + to);
+        });
     };
 
     f16v o[kD];
@@ -324,7 +350,7 @@ __global__ void __launch_bounds__(64 * kRows * kKeys, kRows == 1 && DK > 128 ? 1
 #pragma unroll
                 for (int i = 0; i < kIds; i += 64) ids[i + lane] = table[min(p0 + i + lane, last_place)];
             }
-            issue(t, buf, [&](int, int place) { return ids[place - ids_from]; });
+            issue(t, buf, [&](int place) { return ids[place - ids_from]; });
         };
         if (t0 < t1) fetch(t0, 0);
         if (t0 + kKeys < t1) fetch(t0 + kKeys, 1);
@@ -337,26 +363,22 @@ __global__ void __launch_bounds__(64 * kRows * kKeys, kRows == 1 && DK > 128 ? 1
         }
     } else {
         // One tile on the way, and the page ids of the one behind it
-        int ids[kLoads];
-        auto fetch_ids = [&](int t) {
-#pragma unroll
-            for (int i = 0; i < kLoads; ++i) ids[i] = table[page_of(p, key_of(t, i))];
-        };
-        auto id_of = [&](int i, int) { return ids[i]; };
+        int id = 0;
+        auto fetch_id = [&](int t) { id = table[page_of(p, own_key(t))]; };
+        auto id_of = [&](int) { return id; };
         if (t0 < t1) {
-            fetch_ids(t0);
+            fetch_id(t0);
             issue(t0, 0, id_of);
-            if (t0 + 1 < t1) fetch_ids(t0 + 1);
+            if (t0 + 1 < t1) fetch_id(t0 + 1);
         }
         int buf = 0;
         for (int t = t0; t < t1; ++t, buf ^= 1) {
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); // tile t, and the pages of the next
-#pragma unroll
-            for (int i = 0; i < kLoads; ++i) asm volatile("" : "+v"(ids[i]));   // (nothing of them is waited for among the loads below)
+            asm volatile("" : "+v"(id));                     // (it is not waited for again behind the loads below)
             __syncthreads();                                 // everyone's part of tile t is there, and tile t - 1 has been read
             if (t + 1 < t1) {
                 issue(t + 1, buf ^ 1, id_of);
-                if (t + 2 < t1) fetch_ids(t + 2);
+                if (t + 2 < t1) fetch_id(t + 2);
             }
             work(t, buf);
         }
@@ -519,7 +541,7 @@ Plan plan_of(const sd_attention &a)
     p.dk = D <= 64 ? 64 : D <= 96 ? 96 : D <= 128 ? 128 : D <= 192 ? 192 : 256;
     const bool many = rows > 48 * a.B;
     p.rows = many ? 128 : 32;
-    p.tiles = (int)(rows / p.rows + a.B);
+    p.tiles = (int)(rows / p.rows + a.B) | 1;              // (odd: the splits of a tile go to different dies)
     const int64_t step = many ? (p.dk <= 128 ? 64 : 32) : (p.dk <= 128 ? 2 : 1) * 32;   // keys
     // enough workgroups for the chip, as far as the longest context allows
     const int64_t there = (rows / p.rows > a.B ? rows / p.rows : a.B) * a.cache.heads;
@@ -536,26 +558,32 @@ Plan plan_of(const sd_attention &a)
 // parts, (maximum, sum) of each, and the number of parts of a row
 size_t part_bytes(const sd_attention &a, const Plan &p) { return p.splits > 1 ? (size_t)a.tokens * a.Hq * ((size_t)p.splits * (a.cache.D + 2) + 1) * 4 : 0; }
 
-template <typename T, int DK> void launch(const Attend &p, const Plan &plan, hipStream_t st)
+template <typename T, int DK, bool kFull> void launch(const Attend &p, const Plan &plan, hipStream_t st)
 {
-    const dim3 grid((unsigned)(p.a.cache.heads * plan.tiles), (unsigned)plan.splits);
+    const int64_t items = (int64_t)plan.tiles * plan.splits;
+    const dim3 grid((unsigned)(p.a.cache.heads * (plan.rows == 128 ? items : (items + 7) / 8 * 8)));
     constexpr int kPitch = Shape<DK>::kPitch, kKeys = DK <= 128 ? 2 : 1, KT = DK <= 128 ? 64 : 32;
     if (plan.rows == 128) {
         constexpr int bytes = 4 * KT * kPitch;
-        hipLaunchKernelGGL((sd_attend_kernel<T, DK, 4, 1, KT>), grid, dim3(256), bytes, st, p);
+        hipLaunchKernelGGL((sd_attend_kernel<T, DK, kFull, 4, 1, KT>), grid, dim3(256), bytes, st, p);
     } else {
         constexpr int bytes = kKeys * (4 * 32 * kPitch + 4 * kIds);
         static_assert(kKeys * (64 + 32 * (DK + 4)) * 4 <= kKeys * 4 * 32 * kPitch, "the join has room");
-        static const hipError_t once = hipFuncSetAttribute(reinterpret_cast<const void *>(sd_attend_kernel<T, DK, 1, kKeys, 32>),
+        static const hipError_t once = hipFuncSetAttribute(reinterpret_cast<const void *>(sd_attend_kernel<T, DK, kFull, 1, kKeys, 32>),
                                                            hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
         (void)once;
-        hipLaunchKernelGGL((sd_attend_kernel<T, DK, 1, kKeys, 32>), grid, dim3(64 * kKeys), bytes, st, p);
+        hipLaunchKernelGGL((sd_attend_kernel<T, DK, kFull, 1, kKeys, 32>), grid, dim3(64 * kKeys), bytes, st, p);
     }
     if (plan.splits > 1) {
         const int64_t rows = p.a.tokens * p.a.Hq;
         if (plan.splits > 8) hipLaunchKernelGGL((sd_join_kernel<T, 256>), dim3((unsigned)rows), dim3(256), 0, st, p);
         else hipLaunchKernelGGL((sd_join_kernel<T, 64>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, p);
     }
+}
+template <typename T, int DK> void launch(const Attend &p, const Plan &plan, hipStream_t st)
+{
+    if (p.a.cache.D == DK) launch<T, DK, true>(p, plan, st);
+    else launch<T, DK, false>(p, plan, st);
 }
 template <typename T> void launch(const Attend &p, const Plan &plan, hipStream_t st)
 {
