@@ -107,7 +107,7 @@ typedef struct {
     int64_t B, page;              /* requests; tokens of a page */
     int64_t width, table_stride;  /* entries of a table row; elements from row to row */
     int64_t pool;                 /* pages there are = entries of `free` */
-    int64_t tokens;               /* entries of slot_out and pos_out: sum of add; tokens past them are not written */
+    int64_t tokens;               /* entries of slot_out and pos_out: the sum of add, or more (the rest gets -1), or fewer (tokens past them are left out) */
     const int32_t *pages;         /* [B] pages held */
     const int32_t *length;        /* [B] tokens that were valid before the last step's chunk */
     const int32_t *accepted;      /* [B] accepted drafts of the last step; NULL: length is what is valid */

@@ -444,6 +444,14 @@ def _want(t, name, dtype, n):
     return t.data_ptr()
 
 
+def _want_all(dtype, n, names, *tensors):
+    """The same of several arrays of n entries, without their addresses."""
+    for t in tensors:
+        if t.dtype is not dtype or t.numel() != n or not t.is_contiguous() or not t.is_cuda:
+            for name, u in zip(names.split(), tensors):
+                _want(u, name, dtype, n)
+
+
 def _rows(t, name, dtype, shape):
     """Device address of a tensor whose last dimension is whole; the others may have any stride."""
     if t.dtype is not dtype or t.shape != shape or not t.is_cuda or (t.stride(-1) != 1 and shape[-1] > 1):
@@ -458,11 +466,12 @@ def sd_pages(pages, length, add, table, free, nfree, page, pages_out, length_out
     written (tokens: the sum of add).  Asynchronous."""
     B, width = table.shape
     T, pool, i32 = slot_out.numel(), free.numel(), (_SD_DTYPE or _sd_types())["i32"]
-    step = SdPageStep(B, page, width, table.stride(0) if B > 1 else width, pool, T, _want(pages, "pages", i32, B), _want(length, "length", i32, B),
-                      None if accepted is None else _want(accepted, "accepted", i32, B), _want(add, "add", i32, B),
-                      _want(nfree, "nfree", i32, 1), _rows(table, "table", i32, (B, width)), _want(free, "free", i32, pool),
-                      _want(pages_out, "pages_out", i32, B), _want(length_out, "length_out", i32, B), _want(kv_out, "kv_out", i32, B),
-                      _want(nfree_out, "nfree_out", i32, 1), _want(cu_out, "cu_out", i32, B + 1), _want(slot_out, "slot_out", i32, T),
+    _want_all(i32, B, "pages length add pages_out length_out kv_out", pages, length, add, pages_out, length_out, kv_out)
+    _want_all(i32, 1, "nfree nfree_out", nfree, nfree_out)
+    step = SdPageStep(B, page, width, table.stride(0) if B > 1 else width, pool, T, pages.data_ptr(), length.data_ptr(),
+                      None if accepted is None else _want(accepted, "accepted", i32, B), add.data_ptr(), nfree.data_ptr(),
+                      _rows(table, "table", i32, (B, width)), _want(free, "free", i32, pool), pages_out.data_ptr(), length_out.data_ptr(),
+                      kv_out.data_ptr(), nfree_out.data_ptr(), _want(cu_out, "cu_out", i32, B + 1), _want(slot_out, "slot_out", i32, T),
                       _want(pos_out, "pos_out", i32, T))
     rc = lib().sd_pages(C.byref(step), _stream_ptr(stream))
     if rc != 0:

@@ -64,6 +64,17 @@ __device__ __forceinline__ f2 halves(float x)
     return f2{__uint_as_float(r[0]), __uint_as_float(r[1])};
 }
 
+// the next `n` instructions of a kind (0x8 matrix products, 0x100 reads of LDS), as the compiler orders them
+template <int MASK> __device__ __forceinline__ void order(int n)
+{
+    switch (n) {
+        case 1: __builtin_amdgcn_sched_group_barrier(MASK, 1, 0); break;
+        case 2: __builtin_amdgcn_sched_group_barrier(MASK, 2, 0); break;
+        case 4: __builtin_amdgcn_sched_group_barrier(MASK, 4, 0); break;
+        case 8: __builtin_amdgcn_sched_group_barrier(MASK, 8, 0); break;
+        default: break;
+    }
+}
 // f(0), f(1), .. f(N - 1), each with its number as a type
 template <int N, int I = 0, typename F> __device__ __forceinline__ void unroll(F f)
 {
@@ -75,8 +86,8 @@ template <int N, int I = 0, typename F> __device__ __forceinline__ void unroll(F
 // an address from lane I of each 16 lanes (kSides = 2: from lane 2 I for the first eight of them, lane 2 I + 1 for the others)
 template <int I, int kSides> __device__ __forceinline__ int from_lane(int x)
 {
-    if constexpr (kSides == 1) return __builtin_amdgcn_update_dpp(0, x, 0x150 + I, 0xF, 0xF, false);                 // row_newbcast
-    else return __builtin_amdgcn_update_dpp(__builtin_amdgcn_update_dpp(0, x, 0x150 + 2 * I, 0xF, 0xF, false), x, 0x150 + 2 * I + 1, 0xF, 0xC, false);
+    if constexpr (kSides == 1) return __builtin_amdgcn_mov_dpp(x, 0x150 + I, 0xF, 0xF, false);                       // row_newbcast
+    else return __builtin_amdgcn_update_dpp(__builtin_amdgcn_mov_dpp(x, 0x150 + 2 * I, 0xF, 0xF, false), x, 0x150 + 2 * I + 1, 0xF, 0xC, false);
 }
 template <int I, int kSides> __device__ __forceinline__ const char *from_lane(const char *x)
 {
@@ -107,14 +118,16 @@ __device__ __forceinline__ void load_to_lds(const char *src, unsigned to)
 }
 __device__ __forceinline__ unsigned lds_address(const void *p) { return (unsigned)(uintptr_t)(const __attribute__((address_space(3))) void *)p; }
 
-// Tile x of all requests' rows: those of request b start at floor(cu[b] * G / tile) + b, which is known without a sum over
-// the requests and leaves every one as many as it needs.  Returns the request (by the lanes of a wavefront).
-__device__ __forceinline__ int request_of(const int32_t *cu, int B, int G, int tile, int x, int lane)
+// Tiles of rows are numbered over all requests without a sum over the requests' own numbers of them: floor(cu[b] G / tile), with `each` one
+// more for every request before, leaves request b at least its whole tiles, with `each` its last one too.
+__device__ __forceinline__ int tile_before(int first, int G, int tile, bool each, int b) { return (int)((unsigned)(first * G) / (unsigned)tile) + (each ? b : 0); }
+// the last request with tile_before <= x, by the lanes of a wavefront
+__device__ __forceinline__ int request_of(const int32_t *cu, int B, int G, int tile, bool each, int x, int lane)
 {
     int lo = 0, n = B;
     while (n > 1) {
         const int step = (n + 63) / 64, b = lo + lane * step;
-        const bool in = lane * step < n && (int)((unsigned)(cu[b] * G) / (unsigned)tile) + b <= x;
+        const bool in = lane * step < n && tile_before(cu[b], G, tile, each, b) <= x;
         const unsigned long long mask = __ballot(in);
         const int last = mask ? 63 - __builtin_clzll(mask) : 0;
         n = min(step, n - last * step);
@@ -168,7 +181,7 @@ template <int DK> struct Shape {
 };
 
 template <typename T, int DK, bool kFull, int kRows, int kKeys, int KT>
-__global__ void __launch_bounds__(64 * kRows * kKeys, kRows == 1 && DK > 128 ? 1 : 2) sd_attend_kernel(const Attend p)
+__global__ void __launch_bounds__(64 * kRows * kKeys, DK > 192 || (kRows == 1 && DK > 128) ? 1 : 2) sd_attend_kernel(const Attend p)
 {
     static_assert(kRows == 1 || kKeys == 1, "wavefronts differ in rows or in keys");
     constexpr bool kOwn = kRows == 1;                        // a wavefront has keys of its own
@@ -188,14 +201,17 @@ __global__ void __launch_bounds__(64 * kRows * kKeys, kRows == 1 && DK > 128 ? 1
     // most keys first.  Decoding, where keys are read once: the heads of a range of keys one after the other on one die, so that the pieces of a token's
     // row are fetched at about the same time.
     const unsigned heads = (unsigned)a.cache.heads, turn = kOwn ? blockIdx.x / 8 : blockIdx.x, item = kOwn ? turn / heads * 8 + blockIdx.x % 8 : turn / heads;
-    const int kh = turn % heads, split = item / (unsigned)p.row_tiles, x = p.row_tiles - 1 - (int)(item % (unsigned)p.row_tiles);
+    const int kh = turn % heads, split = item / (unsigned)p.row_tiles, from_first = item % (unsigned)p.row_tiles, x = kOwn ? from_first : p.row_tiles - 1 - from_first;
     if (split >= p.splits) return;
     const int D = kFull ? DK : (int)a.cache.D, G = p.G, page = (int)a.cache.page;
 
-    const int b = request_of(a.cu, (int)a.B, G, kBM, x, lane);
+    // Chunks: the tiles of request b start at floor(cu[b] G / kBM) + b.  Decoding, where nearly every request has one tile: the first B tiles are the
+    // requests' first ones, known without a search, and their further ones start at B + floor(cu[b] G / kBM).
+    const int B = (int)a.B, y = kOwn ? x - B : x;
+    const int b = y < 0 ? x : request_of(a.cu, B, G, kBM, !kOwn, y, lane);
     const Rows rq = rows_of(a, b);
-    const int row0 = (x - ((int)((unsigned)(rq.first * G) / (unsigned)kBM) + b)) * kBM, rows = rq.m * G;
-    if (row0 < 0 || row0 >= rows) return;
+    const int row0 = y < 0 ? 0 : (y - tile_before(rq.first, G, kBM, !kOwn, b) + (kOwn ? 1 : 0)) * kBM, rows = rq.m * G;
+    if (row0 < (kOwn && y >= 0 ? kBM : 0) || row0 >= rows) return;
     const int tok0 = row0 / G, tok1 = (min(row0 + kBM, rows) - 1) / G;
     const Span sp = span_of(a, rq, tok0, tok1, KT * kKeys, p.splits, p.min_steps);
     if (split >= max(sp.used, 1)) return;
@@ -240,7 +256,9 @@ __global__ void __launch_bounds__(64 * kRows * kKeys, kRows == 1 && DK > 128 ? 1
     // (places that none of the tile's rows sees get a key that one does see, so that a zero weight never meets what a page happens to hold)
     auto key_in = [&](int key) { return min(max(key, first_key), last_key); };
     auto own_key = [&](int t) { return key_in(t * KT + own_row); };
-    const unsigned kto = __builtin_amdgcn_readfirstlane(lds_address(kbuf)), vto = __builtin_amdgcn_readfirstlane(lds_address(vbuf));
+    unsigned kto = __builtin_amdgcn_readfirstlane(lds_address(kbuf));
+    asm("" : "+s"(kto));                                     // (not worked out again for each load)
+    const unsigned vto = kto + 2 * kTile;
     auto issue = [&](int t, int buf, auto page_id) {
         const int key = own_key(t), place = page_of(p, key), at = key - place * page;
         const int64_t id = min(max(page_id(place), 0), (int)a.cache.pages - 1);
@@ -269,25 +287,51 @@ __global__ void __launch_bounds__(64 * kRows * kKeys, kRows == 1 && DK > 128 ? 1
         const int key0 = t * KT;
         if (key0 >= any_to || key0 + KT <= any_from) return;
         const char *kt = kbuf + buf * kTile, *vt = vbuf + buf * kTile;
+        // Scores.  Fragments of the keys are read kAhead before they are used: read as they are needed, each product would wait out LDS's latency.
+        constexpr int kFrags = kQ * kBlocks, kAhead = kFrags < 8 ? kFrags : 8;
+        auto k_frag = [&](int f) {
+            const int row = 32 * (f % kBlocks) + col;
+            return *reinterpret_cast<const u4 *>(kt + row * S::kPitch + 16 * S::k_at(row, 2 * (f / kBlocks) + half));
+        };
         f16v s[kBlocks];
 #pragma unroll
-        for (int n = 0; n < kBlocks; ++n) {
+        for (int n = 0; n < kBlocks; ++n)
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[n][r] = 0.f;
+        u4 kf[kAhead];
 #pragma unroll
-            for (int c = 0; c < kQ; ++c) {
-                const int row = 32 * n + col;
-                s[n] = mfma<T>(*reinterpret_cast<const u4 *>(kt + row * S::kPitch + 16 * S::k_at(row, 2 * c + half)), q[c], s[n]);
-            }
+        for (int f = 0; f < kAhead; ++f) kf[f] = k_frag(f);
+#pragma unroll
+        for (int f = 0; f < kFrags; ++f) {
+            s[f % kBlocks] = mfma<T>(kf[f % kAhead], q[f / kBlocks], s[f % kBlocks]);
+            if (f + kAhead < kFrags) kf[f % kAhead] = k_frag(f + kAhead);
+        }
+        // Values, 16 keys (a part) at a time: this lane's are 16 part + 4 half + (0..3) and those + 8, at d = 32 dblock + col; a part ahead
+        const int vrow = 4 * half + ((lane & 15) >> 2), vpiece = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1), voff = 8 * (lane & 1);
+        auto v_frag = [&](int part, int d) {
+            const int r0 = 16 * part + vrow, r1 = r0 + 8;
+            const char *x0 = vt + r0 * S::kPitch + 16 * S::v_at(r0, 4 * d + vpiece) + voff;
+            const char *x1 = vt + r1 * S::kPitch + 16 * S::v_at(r1, 4 * d + vpiece) + voff;
+            const u2 v0 = __builtin_bit_cast(u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4 *)x0));
+            const u2 v1 = __builtin_bit_cast(u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4 *)x1));
+            return u4{v0[0], v0[1], v1[0], v1[1]};
+        };
+        u4 vf[2][kD];
+#pragma unroll
+        for (int d = 0; d < kD; ++d) vf[0][d] = v_frag(0, d);
+        order<0x100>(kAhead);
+#pragma unroll
+        for (int f = 0; f < kFrags; ++f) {
+            order<0x8>(1);
+            order<0x100>(f + kAhead < kFrags ? 1 : f - (kFrags - kAhead) < 2 * kD ? 1 : 0);
         }
         if (key0 < whole_from || key0 + KT > whole_to) {
+            const int base = key0 + 4 * half - from;
+            const unsigned seen = (unsigned)(to - from);
 #pragma unroll
             for (int n = 0; n < kBlocks; ++n)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int key = key0 + 32 * n + 8 * (r >> 2) + 4 * half + (r & 3);
-                    s[n][r] = key >= from && key < to ? s[n][r] : -INFINITY;
-                }
+                for (int r = 0; r < 16; ++r) s[n][r] = (unsigned)(base + 32 * n + 8 * (r >> 2) + (r & 3)) < seen ? s[n][r] : -INFINITY;
         }
         float most = s[0][0];
 #pragma unroll
@@ -308,33 +352,31 @@ __global__ void __launch_bounds__(64 * kRows * kKeys, kRows == 1 && DK > 128 ? 1
                 for (int r = 0; r < 16; ++r) o[d][r] *= back;
         }
         const float ref = top == -INFINITY ? 0.f : top;
-        unsigned w[kBlocks][8];
+        // weights of part i: registers 8 (i % 2) .. + 7 of block i / 2; those of the next part are made while the products of this one run
+        auto weigh = [&](int part) {
+            u4 w;
 #pragma unroll
-        for (int n = 0; n < kBlocks; ++n)
-#pragma unroll
-            for (int r = 0; r < 16; r += 2) {
-                const float w0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][r], p.scale, -ref));
-                const float w1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][r + 1], p.scale, -ref));
+            for (int r = 0; r < 4; ++r) {
+                const float w0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[part / 2][8 * (part % 2) + 2 * r], p.scale, -ref));
+                const float w1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[part / 2][8 * (part % 2) + 2 * r + 1], p.scale, -ref));
                 sum += w0 + w1;
-                w[n][r / 2] = pack<T>(w0, w1);
+                w[r] = pack<T>(w0, w1);
             }
-        // 16 keys at a time: this lane's are 16 c + 4 half + (0..3) and those + 8, at d = 32 dblock + col
-        const int vrow = 4 * half + ((lane & 15) >> 2), vpiece = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1), voff = 8 * (lane & 1);
+            return w;
+        };
+        u4 w = weigh(0);
 #pragma unroll
-        for (int n = 0; n < kBlocks; ++n)
+        for (int part = 0; part < 2 * kBlocks; ++part) {
+            u4 next = w;
+            if (part + 1 < 2 * kBlocks) {
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                const u4 weights = {w[n][4 * c], w[n][4 * c + 1], w[n][4 * c + 2], w[n][4 * c + 3]};
-                const int r0 = 32 * n + 16 * c + vrow, r1 = r0 + 8;
-#pragma unroll
-                for (int d = 0; d < kD; ++d) {
-                    const char *x0 = vt + r0 * S::kPitch + 16 * S::v_at(r0, 4 * d + vpiece) + voff;
-                    const char *x1 = vt + r1 * S::kPitch + 16 * S::v_at(r1, 4 * d + vpiece) + voff;
-                    const u2 v0 = __builtin_bit_cast(u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4 *)x0));
-                    const u2 v1 = __builtin_bit_cast(u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4 *)x1));
-                    o[d] = mfma<T>(u4{v0[0], v0[1], v1[0], v1[1]}, weights, o[d]);
-                }
+                for (int d = 0; d < kD; ++d) vf[(part + 1) % 2][d] = v_frag(part + 1, d);
+                next = weigh(part + 1);
             }
+#pragma unroll
+            for (int d = 0; d < kD; ++d) o[d] = mfma<T>(vf[part % 2][d], w, o[d]);
+            w = next;
+        }
     };
 
     if (kOwn) {
@@ -458,29 +500,42 @@ __global__ void __launch_bounds__(64 * kRows * kKeys, kRows == 1 && DK > 128 ? 1
     }
 }
 
-// The parts of rows whose keys were split: kLanes lanes a row (a workgroup, or a wavefront where parts are few), D / 4 of them to a
-// part.  Their number was left by the workgroups of the first split, so that nothing of the requests is looked up again.
+// The parts of rows whose keys were split: kLanes lanes a row (a wavefront for up to 8 parts, a workgroup for up to 256), D / 4 of them to a
+// part.  The number of parts was left by the workgroups of the first split, so that nothing of the requests is looked up again; a row is two
+// dependent trips to memory.
 template <typename T, int kLanes> __global__ void __launch_bounds__(256) sd_join_kernel(const Attend p)
 {
-    constexpr int kRows = 256 / kLanes;
-    __shared__ float w_sh[kRows][256];
+    constexpr int kRows = 256 / kLanes, kParts = kLanes == 64 ? 8 : 256;
+    __shared__ float w_sh[kRows][kParts];
     __shared__ float4 v_sh[kRows][kLanes];
     const sd_attention &a = p.a;
     const int tid = threadIdx.x % kLanes, group = threadIdx.x / kLanes, lane = threadIdx.x & 63;
     const int64_t rows = a.tokens * a.Hq, orow = (int64_t)blockIdx.x * kRows + group;
     const int D = (int)a.cache.D;
-    const int used = orow < rows && orow / a.Hq < a.cu[a.B] ? min(p.used[orow], p.splits) : 0;   // (tokens of no request have none)
+    const f2 *const ml = reinterpret_cast<const f2 *>(p.part_ml) + orow;
+    f2 mine[kParts < 64 ? 1 : kParts / 64];                  // (parts that were not written are left out below)
+    int used = 0;
+    if (orow < rows) {
+#pragma unroll
+        for (int i = 0; i < (kParts < 64 ? 1 : kParts / 64); ++i)
+            if (lane + 64 * i < p.splits) mine[i] = ml[(lane + 64 * i) * rows];
+        used = orow / a.Hq < a.cu[a.B] ? min(p.used[orow], p.splits) : 0;   // (tokens of no request have none)
+    }
     if (used <= 1 && kLanes > 64) return;                    // (all of a workgroup; otherwise it has a barrier to reach)
-    const float *ml = p.part_ml + 2 * orow;
     // maximum and sum (every wavefront of the row by itself), and the parts' weights
     float top = -INFINITY, sum = 0.f;
-    for (int s = lane; s < used; s += 64) top = fmaxf(top, ml[2 * s * rows]);
+#pragma unroll
+    for (int i = 0; i < (kParts < 64 ? 1 : kParts / 64); ++i) {
+        if (lane + 64 * i >= used) mine[i] = f2{-INFINITY, 0.f};
+        top = fmaxf(top, mine[i][0]);
+    }
 #pragma unroll
     for (int sh = 32; sh >= 1; sh >>= 1) top = fmaxf(top, __shfl_xor(top, sh));
-    for (int s = lane; s < used; s += 64) {
-        const float m = ml[2 * s * rows], w = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
-        sum += w == 0.f ? 0.f : w * ml[2 * s * rows + 1];
-        w_sh[group][s] = w;                                  // (the same from every wavefront of the row)
+#pragma unroll
+    for (int i = 0; i < (kParts < 64 ? 1 : kParts / 64); ++i) {
+        const float w = mine[i][0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mine[i][0] - top);
+        if (w != 0.f) sum += w * mine[i][1];
+        if (lane + 64 * i < kParts) w_sh[group][lane + 64 * i] = w;     // (the same from every wavefront of the row)
     }
 #pragma unroll
     for (int sh = 32; sh >= 1; sh >>= 1) sum += __shfl_xor(sum, sh);
@@ -489,11 +544,16 @@ template <typename T, int kLanes> __global__ void __launch_bounds__(256) sd_join
     float4 v{0.f, 0.f, 0.f, 0.f};
     if (s0 < parts) {
         const float *src = p.part + orow * D + d;
-#pragma unroll 4
-        for (int s = s0; s < used; s += parts) {
-            const float w = w_sh[group][s];
-            const float4 e = *reinterpret_cast<const float4 *>(src + (int64_t)s * rows * D);
-            if (w != 0.f) { v.x += w * e.x; v.y += w * e.y; v.z += w * e.z; v.w += w * e.w; }
+        for (int s1 = s0; s1 < used; s1 += 8 * parts) {
+            float4 e[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (s1 + i * parts < used) e[i] = *reinterpret_cast<const float4 *>(src + (int64_t)(s1 + i * parts) * rows * D);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float w = s1 + i * parts < used ? w_sh[group][s1 + i * parts] : 0.f;
+                if (w != 0.f) { v.x += w * e[i].x; v.y += w * e[i].y; v.z += w * e[i].z; v.w += w * e[i].w; }
+            }
         }
     }
     v_sh[group][tid] = v;
@@ -547,7 +607,7 @@ Plan plan_of(const sd_attention &a)
     const int64_t there = (rows / p.rows > a.B ? rows / p.rows : a.B) * a.cache.heads;
     int64_t longest = a.width * a.cache.page;
     if (a.window > 0 && a.window + p.rows / G + 1 < longest) longest = a.window + p.rows / G + 1;
-    int64_t splits = many ? (there < 256 ? (512 + there - 1) / there : 1) : (2048 + there - 1) / there;
+    int64_t splits = there < 256 || !many ? (512 + there - 1) / there : 1;
     p.min_steps = there >= 256 ? 16 : there >= 64 ? 4 : 2;
     const int64_t most = (longest + p.min_steps * step - 1) / (p.min_steps * step);
     if (splits > most) splits = most;

@@ -1,33 +1,41 @@
-// Block tables and slot maps of a served step, and the write of new keys and values into a paged cache.
+// Block tables and slot maps of a served step.
 //
 // sd_pages is integer bookkeeping: per request the pages it needs and the pages it gives back, three
 // exclusive sums over the requests (new tokens, pages given back, pages taken), and then items that are
-// independent of each other: one per new token, per page taken, per page pushed.  There is nothing to
+// independent of each other: one per four new tokens, per page taken, per page pushed.  There is nothing to
 // stream (a decoding step of 64 requests touches 5 KB), so what counts is the number of launches and of dependent trips
 // to memory: one launch, in which every workgroup sums over all requests by itself (16 KB per input from L2 at
-// most) into LDS and then works its share of the items, finding an item's request by bisection there.  No workgroup
-// waits for another: what one reads (entries held before, the stack below its old top) none writes.
+// most) and keeps what it found of each in LDS, then works its share of the items, finding an item's request by bisection
+// there.  No workgroup waits for another: what one reads (entries held before, the stack below its old top) none writes.
 #include "../../include/specdec.h"
 
 #include <hip/hip_runtime.h>
 
 namespace {
 
-constexpr int kMaxB = SD_MAX_REQUESTS;
+constexpr int kThreads = 256, kWaves = kThreads / 64;
+
+struct Step {
+    sd_page_step s;
+    int page_shift;                // x / page = mulhi(2 x, page_mul) >> page_shift for x < 2^31
+    unsigned page_mul;
+};
+__device__ __forceinline__ int page_of(const Step &p, int x) { return (int)(__umulhi(2u * (unsigned)x, p.page_mul) >> p.page_shift); }
 
 struct Need { int add, back, need, keep, held, want; };
 
 // what request b has, needs and gives back; numbers out of range are clamped
-__device__ __forceinline__ Need need_of(const sd_page_step &s, int b)
+__device__ __forceinline__ Need need_of(const Step &p, int b)
 {
+    const sd_page_step &s = p.s;
     Need r;
-    r.held = min(max(s.pages[b], 0), (int)s.width);
-    const int64_t cap = (int64_t)r.held * s.page;
-    const int64_t more = s.accepted ? (int64_t)max(s.accepted[b], 0) + 1 : 0;
-    r.keep = (int)min((int64_t)max(s.length[b], 0) + more, cap);
-    r.add = min(max(s.add[b], 0), 0x7fffffff / (int)s.B);
-    const int64_t want = ((int64_t)r.keep + r.add + s.page - 1) / s.page;
-    r.want = (int)min(want, s.width + 1);
+    const int pages = s.pages[b], length = s.length[b], accepted = s.accepted ? s.accepted[b] : -1, add = s.add[b];
+    r.held = min(max(pages, 0), (int)s.width);
+    const unsigned more = s.accepted ? (unsigned)max(accepted, 0) + 1 : 0;
+    r.keep = (int)min((unsigned)max(length, 0) + more, (unsigned)(r.held * (int)s.page));
+    r.add = min(max(add, 0), 0x7fffffff / (int)s.B);
+    const int x = (int)min((unsigned)r.keep + (unsigned)r.add, 0x7fffffffu);
+    r.want = x ? min(page_of(p, x - 1) + 1, (int)s.width + 1) : 0;
     r.back = max(r.held - r.want, 0);
     r.need = r.want <= s.width ? max(r.want - r.held, 0) : 0;
     return r;
@@ -54,37 +62,41 @@ __device__ __forceinline__ int find(const int *sum, int B, int x)
     return lo;
 }
 
-__global__ void __launch_bounds__(256) sd_pages_kernel(const sd_page_step s)
+__global__ void __launch_bounds__(kThreads) sd_pages_kernel(const Step p)
 {
-    constexpr int kWaves = 4;
-    __shared__ int cu[kMaxB], back[kMaxB], taken[kMaxB];      // sums over the requests before
+    extern __shared__ int lds[];
     __shared__ int part[3][kWaves];
+    const sd_page_step &s = p.s;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int B = (int)s.B;
-    const int per = (B + 255) / 256;
+    const int B = (int)s.B, page = (int)s.page;
+    int *const cu = lds, *const back = cu + B, *const taken = back + B;      // sums over the requests before
+    int *const keep = taken + B, *const pages = keep + B;                    // tokens kept; pages held, ~pages if refused
+    const int per = (B + kThreads - 1) / kThreads;
 
-    int a = 0, f = 0, t = 0;
-    for (int e = 0; e < per; ++e) {
+    const Need first_need = tid * per < B ? need_of(p, tid * per) : Need{0, 0, 0, 0, 0, 0};
+    int a = first_need.add, f = first_need.back, t = first_need.need;
+    for (int e = 1; e < per; ++e) {
         const int b = tid * per + e;
-        if (b < B) { const Need r = need_of(s, b); a += r.add; f += r.back; t += r.need; }
+        if (b < B) { const Need r = need_of(p, b); a += r.add; f += r.back; t += r.need; }
     }
+    const int nfree = min(max(s.nfree[0], 0), (int)s.pool);
     const int ia = wave_scan(a, lane), iff = wave_scan(f, lane), it = wave_scan(t, lane);
     if (lane == 63) { part[0][wave] = ia; part[1][wave] = iff; part[2][wave] = it; }
     __syncthreads();
-    int ea = ia - a, ef = iff - f, et = it - t, total_back = 0;
+    int ea = ia - a, ef = iff - f, et = it - t, all_add = 0, all_back = 0, all_need = 0;
     for (int w = 0; w < kWaves; ++w) {
         if (w < wave) { ea += part[0][w]; ef += part[1][w]; et += part[2][w]; }
-        total_back += part[1][w];
+        all_add += part[0][w];
+        all_back += part[1][w];
+        all_need += part[2][w];
     }
-    const int pool = (int)s.pool;
-    const int nfree = min(max(s.nfree[0], 0), pool);
-    const int top = min(nfree + total_back, pool);            // of the stack once the surplus pages are on it
+    const int top = min(nfree + all_back, (int)s.pool);       // of the stack once the surplus pages are on it
     for (int e = 0; e < per; ++e) {
         const int b = tid * per + e;
         if (b >= B) break;
-        const Need r = need_of(s, b);
-        cu[b] = ea; back[b] = ef; taken[b] = et;
+        const Need r = e ? need_of(p, b) : first_need;
         const bool served = r.want <= s.width && (r.need == 0 || et + r.need <= top);
+        cu[b] = ea; back[b] = ef; taken[b] = et; keep[b] = r.keep; pages[b] = served ? r.held : ~r.held;
         if (blockIdx.x == 0) {
             s.cu_out[b] = ea;
             if (b == B - 1) s.cu_out[B] = ea + r.add;
@@ -96,50 +108,61 @@ __global__ void __launch_bounds__(256) sd_pages_kernel(const sd_page_step s)
     }
     __syncthreads();
 
-    // what was taken: up to the first request that found too few pages
-    int all_taken;
-    {
-        const Need r = need_of(s, B - 1);
-        all_taken = taken[B - 1] + r.need;
-        if (all_taken > top) {
-            int lo = 0, hi = B - 1;                           // the first request whose sum passes the top
-            while (lo < hi) {
-                const int mid = (lo + hi) >> 1;
-                if ((mid + 1 < B ? taken[mid + 1] : all_taken) > top) hi = mid; else lo = mid + 1;
-            }
-            all_taken = taken[lo];
+    // what was taken: all, or up to the first request that found too few pages
+    int all_taken = all_need;
+    if (all_need > top) {
+        int lo = 0, hi = B - 1;                               // the first request whose sum passes the top
+        while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if ((mid + 1 < B ? taken[mid + 1] : all_need) > top) hi = mid; else lo = mid + 1;
         }
+        all_taken = taken[lo];
     }
     const int left = top - all_taken;
     if (blockIdx.x == 0 && tid == 0) s.nfree_out[0] = left;
 
-    const int step = gridDim.x * 256, first = blockIdx.x * 256 + tid;
+    const int step = gridDim.x * kThreads, first = blockIdx.x * kThreads + tid;
     // entry i of the stack with the surplus pages on it
     auto stack = [&](int i) {
         if (i < nfree) return s.free[i];
         const int b = find(back, B, i - nfree);
-        const int at = need_of(s, b).want + (i - nfree - back[b]);
+        const int held = pages[b] < 0 ? ~pages[b] : pages[b], given = (b + 1 < B ? back[b + 1] : all_back) - back[b];
+        const int at = held - given + (i - nfree - back[b]);
         return at >= 0 && at < s.width ? s.table[b * s.table_stride + at] : -1;
     };
     for (int i = first; i < all_taken; i += step) {
-        const int b = find(taken, B, i);
-        const int at = need_of(s, b).held + i - taken[b];
-        if (at < s.width) s.table[b * s.table_stride + at] = stack(top - 1 - i);
+        const int b = find(taken, B, i), at = pages[b] + i - taken[b];
+        if (at >= 0 && at < s.width) s.table[b * s.table_stride + at] = stack(top - 1 - i);
     }
     for (int i = nfree + first; i < left; i += step) s.free[i] = stack(i);
-    for (int i = first; i < s.tokens; i += step) {
-        const int b = find(cu, B, i);
-        const Need r = need_of(s, b);
-        const bool served = r.want <= s.width && (r.need == 0 || taken[b] + r.need <= top);
-        int slot = -1, pos = -1;
-        if (served && i - cu[b] < r.add) {
-            pos = r.keep + i - cu[b];
-            const int at = pos / (int)s.page;
-            const int page = at < r.held ? s.table[b * s.table_stride + at] : stack(top - 1 - (taken[b] + at - r.held));
-            slot = page * (int)s.page + pos % (int)s.page;
+    for (int64_t i0 = 4ll * first; i0 < s.tokens; i0 += 4ll * step) {
+        int b = find(cu, B, (int)i0), place = -1, id = -1;
+        int slot[4], pos[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int i = (int)i0 + e, was = b;
+            while (b + 1 < B && cu[b + 1] <= i) ++b;
+            const int held = pages[b];
+            const int x = keep[b] + (i - cu[b]), at = page_of(p, x);
+            slot[e] = pos[e] = -1;
+            if (held >= 0 && i < all_add && at < s.width) {
+                if (at != place || b != was) {
+                    place = at;
+                    const int k = top - 1 - (taken[b] + at - held);
+                    id = at < held ? s.table[b * s.table_stride + at] : k >= 0 ? stack(k) : -1;
+                }
+                slot[e] = id * page + (x - at * page);
+                pos[e] = x;
+            }
         }
-        s.slot_out[i] = slot;
-        s.pos_out[i] = pos;
+        if (i0 + 4 <= s.tokens && p.s.tokens % 4 == 0 && ((reinterpret_cast<uintptr_t>(s.slot_out) | reinterpret_cast<uintptr_t>(s.pos_out)) & 15) == 0) {
+            *reinterpret_cast<int4 *>(s.slot_out + i0) = int4{slot[0], slot[1], slot[2], slot[3]};
+            *reinterpret_cast<int4 *>(s.pos_out + i0) = int4{pos[0], pos[1], pos[2], pos[3]};
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (i0 + e < s.tokens) { s.slot_out[i0 + e] = slot[e]; s.pos_out[i0 + e] = pos[e]; }
+        }
     }
 }
 
@@ -164,9 +187,20 @@ extern "C" int sd_pages(const sd_page_step *step, void *hip_stream)
     const int64_t most = 0x7fffffff;
     if (s.B > SD_MAX_REQUESTS || s.page > most || s.width >= most || s.pool > most || s.tokens > most) return SD_EUNSUPPORTED;
     if (s.width * s.page > most || s.pool * s.page > most || s.width * s.B > most) return SD_EUNSUPPORTED;   // (sums are 32 bits)
+    Step p;
+    p.s = s;
+    // x / page for x < 2^31: with h = ceil(log2(page)), floor(x m / 2^(31 + h)), m = floor(2^(31 + h) / page) + 1 <= 2^32 - 1
+    int h = 0;
+    while ((1ll << h) < s.page) ++h;
+    p.page_mul = (unsigned)((1ull << (31 + h)) / (unsigned long long)s.page + 1);
+    p.page_shift = h;
     // a workgroup per 1024 tokens, four to a thread; they also share out the pages
     int64_t grid = (s.tokens + 1023) / 1024;
     grid = grid < 1 ? 1 : grid > 1024 ? 1024 : grid;
-    hipLaunchKernelGGL(sd_pages_kernel, dim3((unsigned)grid), dim3(256), 0, static_cast<hipStream_t>(hip_stream), s);
+    const unsigned bytes = (unsigned)s.B * 5 * sizeof(int);
+    static const hipError_t once = hipFuncSetAttribute(reinterpret_cast<const void *>(sd_pages_kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                                       SD_MAX_REQUESTS * 5 * sizeof(int));
+    (void)once;
+    hipLaunchKernelGGL(sd_pages_kernel, dim3((unsigned)grid), dim3(kThreads), bytes, static_cast<hipStream_t>(hip_stream), p);
     return hipGetLastError() == hipSuccess ? SD_OK : SD_EHIP;
 }

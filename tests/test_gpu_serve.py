@@ -95,6 +95,17 @@ def test_tables_finished_refused_and_repeated():
     assert np.array_equal(few["slot"], want["slot"][:37]) and np.array_equal(few["cu"], want["cu"])
 
 
+@pytest.mark.parametrize("Bn,extra", [(1, 3), (70, 5), (300, 4096)])
+def test_tables_of_a_padded_step(Bn, extra):
+    """More token entries than tokens: the rest has no slot."""
+    rng = np.random.default_rng(Bn)
+    st = _pages_state(rng, Bn, 16, 30, 2000, 200, rng.integers(0, 40, Bn))
+    T = int(st["add"].sum())
+    got, want = _run_pages(st, 16, tokens=T + extra), SO.pages(page=16, **{**st, "nfree": 2000})
+    assert np.array_equal(got["slot"][:T], want["slot"]) and np.array_equal(got["pos"][:T], want["pos"])
+    assert (got["slot"][T:] == -1).all() and (got["pos"][T:] == -1).all()
+
+
 def test_tables_clamp_what_the_host_cannot_see():
     """Lengths, counts and stack heights out of range give some result, inside the arrays."""
     rng = np.random.default_rng(6)
