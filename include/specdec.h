@@ -149,8 +149,10 @@ int sd_cache_store(const sd_cache *cache, const void *k, int64_t k_tok_stride, i
  * tokens: row i stands at position pos = kv[b] - m_b + i and sees the keys j with
  * max(0, pos - window + 1) <= j <= pos (window = 0: from 0 on).  Query head h reads key head h / (Hq / heads).
  *   out = sum_j softmax_j(scale <q, k_j>) v_j,      lse = log sum_j exp(scale <q, k_j>);
- * a row that sees no key (pos < 0) gets out = 0 and lse = -inf.  Keys that no row of a chunk sees are not
- * used, whatever they hold.
+ * a row that sees no key (pos < 0) gets out = 0 and lse = -inf.  Rows of no request (past cu[B]) are not written.
+ * Keys that no row of a chunk sees are not used, whatever they hold.  Of a key that some rows see and others do not (a later
+ * token of the chunk, the edge of the window) those others see nothing if its value is finite; one that is not may turn their results
+ * into NaN too, since a weight of 0 multiplies it.
  * SD_BF16 and SD_F16; scores, softmax and sums are float32, the weights are rounded to the cache's type
  * before they multiply the values.  D a multiple of 8, at most SD_MAX_HEAD_DIM; rows of D elements and all
  * strides 16-byte aligned.

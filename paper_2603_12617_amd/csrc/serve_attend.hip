@@ -118,24 +118,6 @@ __device__ __forceinline__ void load_to_lds(const char *src, unsigned to)
 }
 __device__ __forceinline__ unsigned lds_address(const void *p) { return (unsigned)(uintptr_t)(const __attribute__((address_space(3))) void *)p; }
 
-// Tiles of rows are numbered over all requests without a sum over the requests' own numbers of them: floor(cu[b] G / tile), with `each` one
-// more for every request before, leaves request b at least its whole tiles, with `each` its last one too.
-__device__ __forceinline__ int tile_before(int first, int G, int tile, bool each, int b) { return (int)((unsigned)(first * G) / (unsigned)tile) + (each ? b : 0); }
-// the last request with tile_before <= x, by the lanes of a wavefront
-__device__ __forceinline__ int request_of(const int32_t *cu, int B, int G, int tile, bool each, int x, int lane)
-{
-    int lo = 0, n = B;
-    while (n > 1) {
-        const int step = (n + 63) / 64, b = lo + lane * step;
-        const bool in = lane * step < n && tile_before(cu[b], G, tile, each, b) <= x;
-        const unsigned long long mask = __ballot(in);
-        const int last = mask ? 63 - __builtin_clzll(mask) : 0;
-        n = min(step, n - last * step);
-        lo += last * step;
-    }
-    return lo;
-}
-
 struct Rows { int first, count, m, kv, before; };   // a request's first token, its tokens, keys, and keys before its first token (may be negative)
 __device__ __forceinline__ Rows rows_of(const sd_attention &a, int b)
 {
@@ -148,6 +130,39 @@ __device__ __forceinline__ Rows rows_of(const sd_attention &a, int b)
     r.count = r.m;
     return r;
 }
+// Tile x of all requests' tiles of rows (`skip` of each left out): its request, and which of that request's it is; false past the last.  By the
+// lanes of a wavefront: sums over a 64th of the requests each, then over those one by one.  Exact, so that the workgroups without a tile are the
+// last ones: workgroups go to the parts of a die in turn, and were every other one without work, half of the chip would be.
+struct Tile { int b, at; };
+__device__ __forceinline__ bool tile_of(const sd_attention &a, int G, int tile, int skip, int x, int lane, Tile &out)
+{
+    const int B = (int)a.B;
+    auto tiles = [&](int b) { return max((int)(((unsigned)(rows_of(a, b).m * G) + tile - 1) / (unsigned)tile) - skip, 0); };
+    int lo = 0, n = B;
+    for (;;) {
+        const int chunk = (n + 63) / 64;
+        int count = 0;
+        for (int e = 0; e < chunk; ++e)
+            if (lane * chunk + e < n) count += tiles(lo + lane * chunk + e);
+        int sum = count;
+#pragma unroll
+        for (int sh = 1; sh < 64; sh <<= 1) {
+            const int other = __shfl_up(sum, sh);
+            if (lane >= sh) sum += other;
+        }
+        const unsigned long long past = __ballot(sum > x);
+        if (past == 0) return false;
+        const int at = __builtin_ctzll(past);
+        x -= __builtin_amdgcn_readlane(sum, at) - __builtin_amdgcn_readlane(count, at);
+        lo += at * chunk;
+        if (chunk == 1) break;
+        n = min(chunk, n - at * chunk);
+    }
+    out.b = lo;
+    out.at = x;
+    return true;
+}
+
 // the keys that a token of a request sees
 __device__ __forceinline__ int see_to(const Rows &r, int tok) { return min(max(r.before + tok + 1, 0), r.kv); }
 __device__ __forceinline__ int see_from(const sd_attention &a, const Rows &r, int tok)
@@ -197,21 +212,23 @@ __global__ void __launch_bounds__(64 * kRows * kKeys, DK > 192 || (kRows == 1 &&
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = kRows > 1 ? wave : 0, wk = kRows > 1 ? 0 : wave;
     const int half = lane >> 5, col = lane & 31;
-    // The chip deals workgroups to its eight dies in turn.  Chunks: the tiles of a key head to one die, whose cache then holds its keys, the tiles with
-    // most keys first.  Decoding, where keys are read once: the heads of a range of keys one after the other on one die, so that the pieces of a token's
+    // The chip deals workgroups to its eight dies in turn.  Chunks: a key head's tiles of rows go to one die (of eight heads), whose cache then holds
+    // its keys.  Decoding, where keys are read once: the heads of a range of keys one after the other on one die, so that the pieces of a token's
     // row are fetched at about the same time.
     const unsigned heads = (unsigned)a.cache.heads, turn = kOwn ? blockIdx.x / 8 : blockIdx.x, item = kOwn ? turn / heads * 8 + blockIdx.x % 8 : turn / heads;
-    const int kh = turn % heads, split = item / (unsigned)p.row_tiles, from_first = item % (unsigned)p.row_tiles, x = kOwn ? from_first : p.row_tiles - 1 - from_first;
+    const int kh = turn % heads, split = item / (unsigned)p.row_tiles, x = item % (unsigned)p.row_tiles;
     if (split >= p.splits) return;
     const int D = kFull ? DK : (int)a.cache.D, G = p.G, page = (int)a.cache.page;
 
-    // Chunks: the tiles of request b start at floor(cu[b] G / kBM) + b.  Decoding, where nearly every request has one tile: the first B tiles are the
-    // requests' first ones, known without a search, and their further ones start at B + floor(cu[b] G / kBM).
-    const int B = (int)a.B, y = kOwn ? x - B : x;
-    const int b = y < 0 ? x : request_of(a.cu, B, G, kBM, !kOwn, y, lane);
+    // Decoding, where nearly every request has one tile: the first B tiles are the requests' first ones, known without a search.  Chunks: of a request's
+    // tiles the last, which sees most keys, first.
+    const int B = (int)a.B;
+    Tile tile{x, 0};
+    if (!(kOwn && x < B) && !tile_of(a, G, kBM, kOwn ? 1 : 0, kOwn ? x - B : x, lane, tile)) return;
+    const int b = tile.b;
     const Rows rq = rows_of(a, b);
-    const int row0 = y < 0 ? 0 : (y - tile_before(rq.first, G, kBM, !kOwn, b) + (kOwn ? 1 : 0)) * kBM, rows = rq.m * G;
-    if (row0 < (kOwn && y >= 0 ? kBM : 0) || row0 >= rows) return;
+    const int rows = rq.m * G, row0 = kBM * (!kOwn ? (rows - 1) / kBM - tile.at : x < B ? 0 : tile.at + 1);
+    if (row0 >= rows) return;
     const int tok0 = row0 / G, tok1 = (min(row0 + kBM, rows) - 1) / G;
     const Span sp = span_of(a, rq, tok0, tok1, KT * kKeys, p.splits, p.min_steps);
     if (split >= max(sp.used, 1)) return;
@@ -380,8 +397,8 @@ __global__ void __launch_bounds__(64 * kRows * kKeys, DK > 192 || (kRows == 1 &&
     };
 
     if (kOwn) {
-        // Two tiles on the way.  The wavefront's page ids lie in LDS, kIds of them at a time: a load to registers would be waited for together with
-        // the tiles behind it.
+        // Two tiles on the way: a buffer is filled again as soon as it has been read.  The wavefront's page ids lie in LDS, kIds of them at a time: a
+        // load to registers would be waited for together with the tiles behind it.
         int *const ids = reinterpret_cast<int *>(lds + kKeys * 4 * kTile) + wk * kIds;
         const int last_place = page_of(p, last_key);
         int ids_from = -kIds;
@@ -415,9 +432,10 @@ __global__ void __launch_bounds__(64 * kRows * kKeys, DK > 192 || (kRows == 1 &&
         }
         int buf = 0;
         for (int t = t0; t < t1; ++t, buf ^= 1) {
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); // tile t, and the pages of the next
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");   // tile t, and the pages of the next
             asm volatile("" : "+v"(id));                     // (it is not waited for again behind the loads below)
-            __syncthreads();                                 // everyone's part of tile t is there, and tile t - 1 has been read
+            __builtin_amdgcn_s_barrier();                    // everyone's part of tile t is there, and tile t - 1 has been read
+            asm volatile("" ::: "memory");
             if (t + 1 < t1) {
                 issue(t + 1, buf ^ 1, id_of);
                 if (t + 2 < t1) fetch_id(t + 2);
@@ -428,6 +446,7 @@ __global__ void __launch_bounds__(64 * kRows * kKeys, DK > 192 || (kRows == 1 &&
     {
         const f2 both = halves(sum);
         sum = both[0] + both[1];
+        if (sum != sum) top = INFINITY;                      // (the maximum left it out: no part without it may pass for the whole row)
     }
 
     const bool whole = sp.used <= 1;
@@ -618,22 +637,22 @@ Plan plan_of(const sd_attention &a)
 // parts, (maximum, sum) of each, and the number of parts of a row
 size_t part_bytes(const sd_attention &a, const Plan &p) { return p.splits > 1 ? (size_t)a.tokens * a.Hq * ((size_t)p.splits * (a.cache.D + 2) + 1) * 4 : 0; }
 
+template <typename T, int DK, bool kFull, int kRows, int kKeys, int KT> void launch_shape(const Attend &p, dim3 grid, hipStream_t st)
+{
+    constexpr int tiles = kKeys * 4 * KT * Shape<DK>::kPitch, bytes = tiles + (kRows == 1 ? 4 * kIds * kKeys : 0);
+    static_assert(kKeys == 1 || kKeys * (64 + 32 * (DK + 4)) * 4 <= tiles, "the join has room");
+    const auto kernel = sd_attend_kernel<T, DK, kFull, kRows, kKeys, KT>;
+    static const hipError_t once = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    (void)once;
+    hipLaunchKernelGGL(kernel, grid, dim3(64 * kRows * kKeys), bytes, st, p);
+}
 template <typename T, int DK, bool kFull> void launch(const Attend &p, const Plan &plan, hipStream_t st)
 {
     const int64_t items = (int64_t)plan.tiles * plan.splits;
     const dim3 grid((unsigned)(p.a.cache.heads * (plan.rows == 128 ? items : (items + 7) / 8 * 8)));
-    constexpr int kPitch = Shape<DK>::kPitch, kKeys = DK <= 128 ? 2 : 1, KT = DK <= 128 ? 64 : 32;
-    if (plan.rows == 128) {
-        constexpr int bytes = 4 * KT * kPitch;
-        hipLaunchKernelGGL((sd_attend_kernel<T, DK, kFull, 4, 1, KT>), grid, dim3(256), bytes, st, p);
-    } else {
-        constexpr int bytes = kKeys * (4 * 32 * kPitch + 4 * kIds);
-        static_assert(kKeys * (64 + 32 * (DK + 4)) * 4 <= kKeys * 4 * 32 * kPitch, "the join has room");
-        static const hipError_t once = hipFuncSetAttribute(reinterpret_cast<const void *>(sd_attend_kernel<T, DK, kFull, 1, kKeys, 32>),
-                                                           hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-        (void)once;
-        hipLaunchKernelGGL((sd_attend_kernel<T, DK, kFull, 1, kKeys, 32>), grid, dim3(64 * kKeys), bytes, st, p);
-    }
+    constexpr int kKeys = DK <= 128 ? 2 : 1, KT = DK <= 128 ? 64 : 32;
+    if (plan.rows == 128) launch_shape<T, DK, kFull, 4, 1, KT>(p, grid, st);
+    else launch_shape<T, DK, kFull, 1, kKeys, 32>(p, grid, st);
     if (plan.splits > 1) {
         const int64_t rows = p.a.tokens * p.a.Hq;
         if (plan.splits > 8) hipLaunchKernelGGL((sd_join_kernel<T, 256>), dim3((unsigned)rows), dim3(256), 0, st, p);
