@@ -65,14 +65,18 @@ template <typename T> __device__ __forceinline__ typename Vec<T>::Raw load(const
     typedef Vec<T> E;
     if (x + E::kVec <= V) return *reinterpret_cast<const typename E::Raw *>(row + x);
     typename E::Raw v = E::none();
-    for (int e = 0; e < E::kVec; ++e)
-        if (x + e < V) {
-            if (sizeof(T) == 4) v[e] = __builtin_bit_cast(decltype(v[0] + v[0]), *reinterpret_cast<const unsigned *>(row + x + e));
-            else {
-                const unsigned h = *reinterpret_cast<const uint16_t *>(row + x + e), old = __builtin_bit_cast(unsigned, v[e / 2]);
-                v[e / 2] = __builtin_bit_cast(decltype(v[0] + v[0]), e & 1 ? (old & 0xffffu) | h << 16 : (old & 0xffff0000u) | h);
-            }
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (x + e < V) v[e] = row[x + e];
+    } else {
+        const uint16_t *const h = reinterpret_cast<const uint16_t *>(row) + x;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const unsigned lo = x + 2 * e < V ? h[2 * e] : v[e] & 0xffffu, hi = x + 2 * e + 1 < V ? h[2 * e + 1] : v[e] >> 16;
+            v[e] = hi << 16 | lo;
         }
+    }
     return v;
 }
 // a thread's logits of segment `seg`: raw[c] from place place(seg, c) on

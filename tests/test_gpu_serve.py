@@ -269,6 +269,48 @@ def test_attention_masked_keys_of_a_chunk_do_not_matter():
     assert _torch().equal(out[:50], again[:50]) and not _torch().equal(out[50:], again[50:])
 
 
+@pytest.mark.parametrize("new,kv", [([3], [40]), ([3], [3000]), ([150], [400])])
+def test_attention_numbers_that_are_none_stay_in_sight(new, kv):
+    """A query that is no number gives a row that is none, and a key that is none the rows that see it; the other rows keep their bits."""
+    torch = _torch()
+    b = _Batch(new, kv, 4, 2, 64, 16, "bf16", seed=6)
+    clean, clean_lse = b.gpu()
+    b.wide_q[1, 2, 7] = float("nan")                                  # token 1, query head 1
+    out, lse = b.gpu()
+    assert torch.isnan(out[1, 1]).all() and torch.isnan(lse[1, 1])
+    keep = torch.ones_like(lse, dtype=torch.bool)
+    keep[1, 1] = False
+    assert torch.equal(out[keep], clean[keep]) and torch.equal(lse[keep], clean_lse[keep])
+    b.wide_q[1, 2, 7] = 0.5
+    clean, clean_lse = b.gpu()
+    last = kv[0] - 1                                                  # the last key, key head 1: seen by the last row's heads 2 and 3 alone
+    b.k[int(b.table[0, last // 16]), last % 16, 1, 3] = float("nan")
+    out, lse = b.gpu()
+    assert torch.isnan(out[-1, 2:]).all() and torch.isnan(lse[-1, 2:]).all()
+    assert torch.equal(out[:-1], clean[:-1]) and torch.equal(out[-1, :2], clean[-1, :2]) and torch.equal(lse[:-1], clean_lse[:-1])
+
+
+@pytest.mark.parametrize("Bn,most,Hq", [(65, 3, 2), (300, 9, 4), (4096, 1, 1), (130, 70, 1)])
+def test_attention_of_many_requests(Bn, most, Hq):
+    rng = np.random.default_rng(Bn)
+    new = rng.integers(0, most + 1, Bn).tolist()
+    kv = [int(n + rng.integers(0, 60)) for n in new]
+    _Batch(new, kv, Hq, 1, 64, 16, "f16", seed=Bn).check()
+
+
+def test_attention_of_a_padded_batch():
+    """Rows past the last request's are nobody's: they are left alone, the others' are the same."""
+    torch = _torch()
+    for new, kv in (([2, 3], [2500, 100]), ([90, 60], [200, 300])):
+        b = _Batch(new, kv, 4, 2, 64, 16, "bf16", seed=5)
+        want, _ = b.gpu()
+        extra = torch.ones((11,) + tuple(b.wide_q.shape[1:]), dtype=b.wide_q.dtype)
+        b.wide_q = torch.cat([b.wide_q, extra])
+        b.q = b.wide_q[:, 1:5]
+        out, _ = b.gpu()
+        assert torch.equal(out[:sum(new)], want) and (out[sum(new):] == -7).all()
+
+
 def test_attention_offsets_beyond_32_bits():
     torch = _torch()
     page, Hkv, D = 64, 8, 128
@@ -355,13 +397,29 @@ def _check_verify(d):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
-@pytest.mark.parametrize("k,V", [([4] * 8, 1000), ([0], 7), ([1], 1), ([0, 3, 1, 8, 0], 4099), ([2] * 30, 8192), ([3] * 5, 8193), ([5, 70], 300), ([2, 2], 50257),
+@pytest.mark.parametrize("k,V", [([4] * 8, 1000), ([0], 7), ([1], 1), ([0, 3, 1, 8, 0], 4099), ([1, 0, 2] * 50, 700), ([2] * 30, 8192), ([3] * 5, 8193), ([5, 70], 300), ([2, 2], 50257),
                                  ([1], 262144)])
 @pytest.mark.parametrize("draft", [True, False])
 def test_verified_tokens(dtype, k, V, draft):
     rng = np.random.default_rng(V + len(k))
     print("case", dtype, k[:6], V, draft, flush=True)
     _check_verify(_logits(rng, k, V, dtype, draft, greedy=0.3 if len(k) > 2 else 0.0))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("V", [1, 2, 7, 12, 20, 700, 1003, 8191, 8198])
+@pytest.mark.parametrize("greedy", [False, True])
+def test_every_place_of_a_row_is_read(dtype, V, greedy):
+    """One logit far above the others, at each of the first and last places of a row of any length."""
+    torch = _torch()
+    xs = sorted(set(range(min(V, 10))) | set(range(max(0, V - 18), V)))
+    p = torch.full((len(xs), V), -5.0)
+    p[range(len(xs)), xs] = 30.0
+    none = np.zeros(0, np.int32)
+    d = dict(p=p.to(_dt(dtype)), q=None, tok=none, r=none.astype(np.float32), noise=np.ones((len(xs), V), np.float32),
+             tau=np.full(len(xs), 0.0 if greedy else 1.0, np.float32), cu=np.arange(len(xs) + 1, dtype=np.int32))
+    n, nx = _run_verify(d)
+    assert (n == 0).all() and nx.tolist() == xs
 
 
 def test_verified_tokens_strides_and_streams():
