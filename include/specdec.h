@@ -156,8 +156,8 @@ int sd_cache_store(const sd_cache *cache, const void *k, int64_t k_tok_stride, i
  * SD_BF16 and SD_F16; scores, softmax and sums are float32, the weights are rounded to the cache's type
  * before they multiply the values.  D a multiple of 8, at most SD_MAX_HEAD_DIM; rows of D elements and all
  * strides 16-byte aligned.
- * `ws` (16-byte aligned) needs sd_attend_workspace_bytes; the split of long contexts that it pays for depends
- * on the shapes alone, so equal shapes give equal bits.
+ * `ws` (16-byte aligned) needs sd_attend_workspace_bytes.  It holds parts of rows whose keys are split over workgroups; how
+ * they are split depends on the shapes and lengths alone, so equal calls give equal bits.
  */
 typedef struct {
     sd_cache cache;

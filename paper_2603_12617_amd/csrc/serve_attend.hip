@@ -101,12 +101,13 @@ struct Attend {
     int G, page_shift;             // query heads of a key head; key / page = mulhi(2 key, page_mul) >> page_shift
     unsigned page_mul;
     float scale;                   // scale * log2(e): weights are powers of two
-    int splits, min_steps;         // of keys; steps that a split has at least
-    int row_tiles;                 // tiles of rows there may be
-    int order;                     // decoding, where a wavefront can hold the requests' lengths: so many of the longest come first, then the others, shortest
-                                   // first; 0: as they come
-    float *part, *part_ml;         // [splits][tokens * Hq][D], [splits][tokens * Hq][2]: weighted values, (maximum, sum)
-    int *used;                     // [tokens * Hq] parts of a row
+    int splits, min_steps;         // chunks: parts that a tile's keys are split into at most; steps of keys that a part has at least
+    int row_tiles;                 // chunks: tiles of rows there may be
+    int units, once;               // decoding: workgroups of a key head; so many of them find room at once (0: they are not split to fill it)
+    bool level;                    // decoding: what is far longer than the others is split
+    int pairs;                     // decoding: where all workgroups find room at once, so many come longest first, the others shortest first (0: as they come)
+    float *part, *part_ml;         // [.][D], [.][2]: weighted values, (maximum, sum) of a row's part
+    int4 *info;                    // [tokens * Hq]: how many parts a row has, where its first is, how far apart they are
 };
 
 __device__ __forceinline__ int page_of(const Attend &p, int key) { return (int)(__umulhi(2u * (unsigned)key, p.page_mul) >> p.page_shift); }
@@ -132,14 +133,14 @@ __device__ __forceinline__ Rows rows_of(const sd_attention &a, int b)
     r.count = r.m;
     return r;
 }
-// Tile x of all requests' tiles of rows (`skip` of each left out): its request, and which of that request's it is; false past the last.  By the
+// Tile x of all requests' tiles of rows: its request, and which of that request's it is; false past the last.  By the
 // lanes of a wavefront: sums over a 64th of the requests each, then over those one by one.  Exact, so that the workgroups without a tile are the
 // last ones: workgroups go to the parts of a die in turn, and were every other one without work, half of the chip would be.
 struct Tile { int b, at; };
-__device__ __forceinline__ bool tile_of(const sd_attention &a, int G, int tile, int skip, int x, int lane, Tile &out)
+__device__ __forceinline__ bool tile_of(const sd_attention &a, int G, int tile, int x, int lane, Tile &out)
 {
     const int B = (int)a.B;
-    auto tiles = [&](int b) { return max((int)(((unsigned)(rows_of(a, b).m * G) + tile - 1) / (unsigned)tile) - skip, 0); };
+    auto tiles = [&](int b) { return (int)(((unsigned)(rows_of(a, b).m * G) + tile - 1) / (unsigned)tile); };
     int lo = 0, n = B;
     for (;;) {
         const int chunk = (n + 63) / 64;
@@ -172,18 +173,6 @@ __device__ __forceinline__ int see_from(const sd_attention &a, const Rows &r, in
     return a.window > 0 ? (int)min((int64_t)r.kv, max((int64_t)0, (int64_t)r.before + tok + 1 - a.window)) : 0;
 }
 
-// the request of up to 64 that is the rank-th longest
-__device__ __forceinline__ int by_length(const int32_t *kv, int B, int rank, int lane)
-{
-    const int mine = lane < B ? kv[lane] : 0;
-    int before = 0;
-    for (int j = 0; j < B; ++j) {
-        const int other = __builtin_amdgcn_readlane(mine, j);
-        before += other > mine || (other == mine && j < lane) ? 1 : 0;
-    }
-    return __builtin_ctzll(__ballot(lane < B && before == rank));
-}
-
 // The steps (of `keys` keys) of a tile of rows, and those of one of its splits.
 struct Span { int first, count, per, used; };
 __device__ __forceinline__ Span span_of(const sd_attention &a, const Rows &r, int tok0, int tok1, int keys, int splits, int min_steps)
@@ -195,6 +184,156 @@ __device__ __forceinline__ Span span_of(const sd_attention &a, const Rows &r, in
     s.per = max((s.count + splits - 1) / splits, min_steps);
     s.used = (s.count + s.per - 1) / s.per;
     return s;
+}
+
+constexpr int kMaxParts = 256;     // of a row
+
+// ---- decoding: what a workgroup does ----
+// sums over the lanes up to this one, as lane moves within the wavefront's registers
+template <int CTRL, int ROWS> __device__ __forceinline__ int moved(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xF, false); }
+__device__ __forceinline__ int scan(int v)
+{
+    v += moved<0x111, 0xF>(v);      // row_shr:1
+    v += moved<0x112, 0xF>(v);
+    v += moved<0x114, 0xF>(v);
+    v += moved<0x118, 0xF>(v);
+    v += moved<0x142, 0xA>(v);      // row_bcast:15: rows 1, 3 += the end of the row before
+    v += moved<0x143, 0xC>(v);      // row_bcast:31: rows 2, 3 += the end of row 1
+    return v;
+}
+__device__ __forceinline__ int total(int v) { return __builtin_amdgcn_readlane(scan(v), 63); }
+__device__ __forceinline__ int largest(int v)       // of numbers that are not negative
+{
+    v = max(v, moved<0x111, 0xF>(v));
+    v = max(v, moved<0x112, 0xF>(v));
+    v = max(v, moved<0x114, 0xF>(v));
+    v = max(v, moved<0x118, 0xF>(v));
+    v = max(v, moved<0x142, 0xA>(v));
+    v = max(v, moved<0x143, 0xC>(v));
+    return __builtin_amdgcn_readlane(v, 63);
+}
+__device__ __forceinline__ float total(float v)
+{
+    auto from = [](float x, auto step) { return __int_as_float(step(__float_as_int(x))); };
+    v += from(v, [](int x) { return moved<0x111, 0xF>(x); });
+    v += from(v, [](int x) { return moved<0x112, 0xF>(x); });
+    v += from(v, [](int x) { return moved<0x114, 0xF>(x); });
+    v += from(v, [](int x) { return moved<0x118, 0xF>(x); });
+    v += from(v, [](int x) { return moved<0x142, 0xA>(x); });
+    v += from(v, [](int x) { return moved<0x143, 0xC>(x); });
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
+
+// A request's tiles of 32 rows, and the steps of keys that they see
+struct Work { int tiles, first, steps; };
+__device__ __forceinline__ Work work_of(const Attend &p, int b, int keys)
+{
+    const Rows r = rows_of(p.a, b);
+    Work w;
+    w.tiles = (r.m * p.G + 31) / 32;
+    w.first = see_from(p.a, r, 0) / keys;
+    w.steps = r.m ? max((see_to(r, r.m - 1) + keys - 1) / keys - w.first, 0) : 0;
+    return w;
+}
+
+// Workgroups of a key head: every tile of a request, times the parts of at most `per` steps that its keys are split into.  Workgroup x
+// works part `split` of tile `tile` of request b; its parts of a tile are `tiles` places apart.
+struct Unit { int b, tile, split, tiles, splits, per, place; Work w; };
+__device__ __forceinline__ bool unit_of(const Attend &p, int x, int keys, int lane, Unit &u)
+{
+    const int B = (int)p.a.B;
+    // A lane holds a request, or of more than 64 the sums over a 64th of them
+    const int chunk = (B + 63) / 64, b0 = lane * chunk;
+    Work w{0, 0, 0};
+    int tiles = 0, longest = 0;
+    float all = 0.f;                                         // steps of all workgroups (tiles' parts), for means
+    for (int e = 0; e < chunk; ++e)
+        if (b0 + e < B) {
+            w = work_of(p, b0 + e, keys);
+            tiles += w.tiles;
+            all += (float)w.tiles * (float)w.steps;
+            if (w.tiles) longest = max(longest, w.steps);
+        }
+    longest = max(largest(longest), 1);
+    int per = longest;                                       // nothing is split
+    if (p.once || p.level) {
+        const int n = total(tiles);
+        all = total(all);
+        const int least = min(max(p.min_steps, (longest + kMaxParts - 1) / kMaxParts), longest);   // (a row is joined from at most kMaxParts)
+        if (n < p.once) {
+            // Parts of one length, as many as find room at once: sum tiles ceil(steps / per) <= once holds for per >= all / (once - n), fails below all / once.
+            int hi = __builtin_amdgcn_readfirstlane(min((int)(all / (float)(p.once - n)) + 1, longest));
+            int lo = __builtin_amdgcn_readfirstlane(min((int)(all / (float)p.once), hi));
+            if (B == 1) hi = (longest + p.once / n - 1) / (p.once / n);
+            else if (chunk == 1)
+                for (int i = 0; i < 5 && lo + 1 < hi; ++i) {
+                    const int mid = (lo + hi) >> 1;
+                    if (total(w.tiles * max((w.steps + mid - 1) / mid, 1)) <= p.once) hi = mid; else lo = mid;
+                }
+            per = max(hi, least);
+        }
+        // What is more than twice as long as the mean is split in any case.
+        if (p.level && p.units > n)
+            per = min(per, max(max((int)(all / (float)(p.units - n)) + 1, (int)(2.f * all / (float)max(n, 1))), least));
+        per = __builtin_amdgcn_readfirstlane(per);
+    }
+    auto splits_of = [&](const Work &v) { return max((v.steps + per - 1) / per, 1); };
+    if (chunk == 1) {
+        int mine = lane < B ? w.tiles * splits_of(w) : 0;
+        if (total(mine) > p.units) {                         // (row offsets that overlap: there may be more tiles than workgroups, but no part without a place)
+            per = longest;
+            mine = w.tiles;
+        }
+        int count = mine, who = lane;
+        if (p.pairs && B > 1) {                              // in the order of their lengths, longest first
+            const int key = w.tiles ? min(w.steps, 1 << 24) * 64 + 63 - lane : 0;
+            int rank = 0;
+            for (int j = 0; j < B; ++j) rank += __builtin_amdgcn_readlane(key, j) > key;
+            // (a request without rows may stand anywhere: the others close up before it)
+            const unsigned long long there = __ballot(w.tiles > 0);
+            if (!w.tiles) rank = __builtin_popcountll(there) + __builtin_popcountll(~there & ((1ull << lane) - 1));
+            count = __builtin_amdgcn_ds_permute(4 * rank, mine);
+            who = __builtin_amdgcn_ds_permute(4 * rank, lane);
+        }
+        const int sum = scan(count), n = __builtin_amdgcn_readlane(sum, 63);
+        if (x >= n) return false;
+        if (n <= 2 * p.pairs && x >= p.pairs) x = n - 1 - (x - p.pairs);
+        const int at = __builtin_ctzll(__ballot(sum > x));
+        u.b = __builtin_amdgcn_readlane(who, at);
+        u.place = x;
+        x -= __builtin_amdgcn_readlane(sum, at) - __builtin_amdgcn_readlane(count, at);
+        u.w = Work{__builtin_amdgcn_readlane(w.tiles, u.b), __builtin_amdgcn_readlane(w.first, u.b), __builtin_amdgcn_readlane(w.steps, u.b)};
+    } else {
+        u.place = x;
+        int count = 0;
+        for (int e = 0; e < chunk; ++e)
+            if (b0 + e < B) { const Work v = work_of(p, b0 + e, keys); count += v.tiles * splits_of(v); }
+        if (total(count) > p.units) {
+            per = longest;
+            count = tiles;
+        }
+        int sum = scan(count);
+        unsigned long long past = __ballot(sum > x);
+        if (past == 0) return false;
+        int at = __builtin_ctzll(past);
+        x -= __builtin_amdgcn_readlane(sum, at) - __builtin_amdgcn_readlane(count, at);
+        const int first = at * chunk;                        // (chunk <= 64: its requests one by one)
+        w = lane < chunk && first + lane < B ? work_of(p, first + lane, keys) : Work{0, 0, 0};
+        count = w.tiles * splits_of(w);
+        sum = scan(count);
+        past = __ballot(sum > x);
+        if (past == 0) return false;
+        at = __builtin_ctzll(past);
+        x -= __builtin_amdgcn_readlane(sum, at) - __builtin_amdgcn_readlane(count, at);
+        u.b = first + at;
+        u.w = Work{__builtin_amdgcn_readlane(w.tiles, at), __builtin_amdgcn_readlane(w.first, at), __builtin_amdgcn_readlane(w.steps, at)};
+    }
+    u.per = per;
+    u.tiles = u.w.tiles;
+    u.splits = splits_of(u.w);
+    u.tile = x % u.tiles;
+    u.split = x / u.tiles;
+    return true;
 }
 
 constexpr int kIds = 256;          // page ids that a wavefront keeps
@@ -230,24 +369,43 @@ __global__ void __launch_bounds__(64 * kRows * kKeys, DK > 192 || (kRows == 1 &&
     // its keys.  Decoding, where keys are read once: the heads of a range of keys one after the other on one die, so that the pieces of a token's
     // row are fetched at about the same time.
     const unsigned heads = (unsigned)a.cache.heads, turn = kOwn ? blockIdx.x / 8 : blockIdx.x, item = kOwn ? turn / heads * 8 + blockIdx.x % 8 : turn / heads;
-    const int kh = turn % heads, split = item / (unsigned)p.row_tiles, x = item % (unsigned)p.row_tiles;
-    if (split >= p.splits) return;
+    const int kh = turn % heads;
     const int D = kFull ? DK : (int)a.cache.D, G = p.G, page = (int)a.cache.page;
 
-    // Decoding, where nearly every request has one tile: the first B tiles are the requests' first ones, known without a search.  Chunks: of a request's
-    // tiles the last, which sees most keys, first.
-    const int B = (int)a.B;
-    Tile tile{x, 0};
-    if (kOwn && p.order && x < B) tile.b = by_length(a.kv, B, x < p.order ? x : B - 1 - (x - p.order), lane);
-    if (!(kOwn && x < B) && !tile_of(a, G, kBM, kOwn ? 1 : 0, kOwn ? x - B : x, lane, tile)) return;
-    const int b = tile.b;
-    const Rows rq = rows_of(a, b);
-    const int rows = rq.m * G, row0 = kBM * (!kOwn ? (rows - 1) / kBM - tile.at : x < B ? 0 : tile.at + 1);
-    if (row0 >= rows) return;
-    const int tok0 = row0 / G, tok1 = (min(row0 + kBM, rows) - 1) / G;
-    const Span sp = span_of(a, rq, tok0, tok1, KT * kKeys, p.splits, p.min_steps);
-    if (split >= max(sp.used, 1)) return;
-    const int t0 = (sp.first + split * sp.per) * kKeys + wk, t1 = (sp.first + min((split + 1) * sp.per, sp.count)) * kKeys;   // tiles t0, t0 + kKeys, .. < t1
+    int b, row0, t0, t1, parts, part_row = 0, part_step = 0, split;      // tiles of keys t0, t0 + kKeys, .. < t1; where the parts of row 0 lie, by rows
+    Rows rq;
+    if (kOwn) {
+        Unit u;
+        if ((int)item >= p.units || !unit_of(p, item, KT * kKeys, lane, u)) return;
+        b = u.b;
+        rq = rows_of(a, b);
+        row0 = kBM * u.tile;
+        split = u.split;
+        parts = u.splits;
+        t0 = u.w.first + split * u.per;
+        t1 = u.w.first + min((split + 1) * u.per, u.w.steps);
+        part_step = u.tiles * (int)heads * kBM;
+        part_row = (u.place * (int)heads + kh) * kBM - split * part_step;
+    } else {
+        split = item / (unsigned)p.row_tiles;
+        Tile tile;
+        if (split >= p.splits || !tile_of(a, G, kBM, item % (unsigned)p.row_tiles, lane, tile)) return;
+        b = tile.b;
+        rq = rows_of(a, b);
+        row0 = kBM * ((rq.m * G - 1) / kBM - tile.at);       // (of a request's tiles the last, which sees most keys, first)
+        t0 = t1 = parts = 0;
+    }
+    const int rows = rq.m * G, tok0 = row0 / G, tok1 = (min(row0 + kBM, rows) - 1) / G;
+    const Span sp = span_of(a, rq, tok0, tok1, KT * kKeys, kOwn ? 1 : p.splits, p.min_steps);
+    if (kOwn) {                                              // (a request's tiles see a little less than all of its keys)
+        t0 = max(t0, sp.first) * kKeys + wk;
+        t1 = min(t1, sp.first + sp.count) * kKeys;
+    } else {
+        if (split >= max(sp.used, 1)) return;
+        parts = sp.used;
+        t0 = (sp.first + split * sp.per) * kKeys;
+        t1 = (sp.first + min((split + 1) * sp.per, sp.count)) * kKeys;
+    }
     const int first_key = see_from(a, rq, tok0), last_key = max(see_to(rq, tok1) - 1, 0);
 
     // this lane's row
@@ -464,8 +622,9 @@ __global__ void __launch_bounds__(64 * kRows * kKeys, DK > 192 || (kRows == 1 &&
         if (sum != sum) top = INFINITY;                      // (the maximum left it out: no part without it may pass for the whole row)
     }
 
-    const bool whole = sp.used <= 1;
+    const bool whole = parts <= 1;
     const int64_t orow = (int64_t)(rq.first + tok) * a.Hq + head;
+    const int64_t first_part = kOwn ? part_row + col : orow, part_stride = kOwn ? part_step : a.tokens * a.Hq, prow = first_part + split * part_stride;
     if (kKeys > 1) {
         // join the wavefronts: maximum, sum and values of each to LDS, then a share of D to each
         constexpr int kP = DK + 4;                           // floats of a row
@@ -505,7 +664,7 @@ __global__ void __launch_bounds__(64 * kRows * kKeys, DK > 192 || (kRows == 1 &&
                     *reinterpret_cast<u2 *>(static_cast<T *>(a.out) + (int64_t)(rq.first + tok) * a.out_tok_stride + (int64_t)head * a.out_head_stride + d) =
                         u2{pack<T>(v.x * inv, v.y * inv), pack<T>(v.z * inv, v.w * inv)};
                 else
-                    *reinterpret_cast<float4 *>(p.part + ((int64_t)split * a.tokens * a.Hq + orow) * D + d) = v;
+                    *reinterpret_cast<float4 *>(p.part + prow * D + d) = v;
             }
         }
     } else if (there) {
@@ -520,69 +679,69 @@ __global__ void __launch_bounds__(64 * kRows * kKeys, DK > 192 || (kRows == 1 &&
                     *reinterpret_cast<u2 *>(static_cast<T *>(a.out) + (int64_t)(rq.first + tok) * a.out_tok_stride + (int64_t)head * a.out_head_stride + at) =
                         u2{pack<T>(o[d][r] * inv, o[d][r + 1] * inv), pack<T>(o[d][r + 2] * inv, o[d][r + 3] * inv)};
                 else
-                    *reinterpret_cast<float4 *>(p.part + ((int64_t)split * a.tokens * a.Hq + orow) * D + at) = float4{o[d][r], o[d][r + 1], o[d][r + 2], o[d][r + 3]};
+                    *reinterpret_cast<float4 *>(p.part + prow * D + at) = float4{o[d][r], o[d][r + 1], o[d][r + 2], o[d][r + 3]};
             }
     }
     if (there && half == 0 && wk == 0) {
-        if (p.splits > 1 && split == 0) p.used[orow] = sp.used;
+        if (p.info && split == 0) p.info[orow] = int4{parts, (int)first_part, (int)part_stride, 0};
         if (whole) {
             if (a.lse) a.lse[orow] = sum != 0.f ? (top + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f : -INFINITY;
         } else {
-            float *ml = p.part_ml + 2 * ((int64_t)split * a.tokens * a.Hq + orow);
+            float *ml = p.part_ml + 2 * prow;
             ml[0] = top; ml[1] = sum;
         }
     }
 }
 
-// The parts of rows whose keys were split: kLanes lanes a row (a wavefront for up to 8 parts, a workgroup for up to 256), D / 4 of them to a
-// part.  The number of parts was left by the workgroups of the first split, so that nothing of the requests is looked up again; a row is two
-// dependent trips to memory.
+// The parts of rows whose keys were split: kLanes lanes a row (a workgroup where rows are few, a wavefront otherwise), D / 4 of them to a
+// part.  How many there are and where was left by the workgroups of the first ones, so that nothing of the requests is looked up again; a row is
+// two dependent trips to memory.
 template <typename T, int kLanes> __global__ void __launch_bounds__(256) sd_join_kernel(const Attend p)
 {
-    constexpr int kRows = 256 / kLanes, kParts = kLanes == 64 ? 8 : 256;
-    __shared__ float w_sh[kRows][kParts];
+    constexpr int kRows = 256 / kLanes, kEach = kMaxParts / 64;
+    __shared__ float w_sh[kRows][kMaxParts];
     __shared__ float4 v_sh[kRows][kLanes];
     const sd_attention &a = p.a;
     const int tid = threadIdx.x % kLanes, group = threadIdx.x / kLanes, lane = threadIdx.x & 63;
     const int64_t rows = a.tokens * a.Hq, orow = (int64_t)blockIdx.x * kRows + group;
     const int D = (int)a.cache.D;
-    const f2 *const ml = reinterpret_cast<const f2 *>(p.part_ml) + orow;
-    f2 mine[kParts < 64 ? 1 : kParts / 64];                  // (parts that were not written are left out below)
-    int used = 0;
-    if (orow < rows) {
-#pragma unroll
-        for (int i = 0; i < (kParts < 64 ? 1 : kParts / 64); ++i)
-            if (lane + 64 * i < p.splits) mine[i] = ml[(lane + 64 * i) * rows];
-        used = orow / a.Hq < a.cu[a.B] ? min(p.used[orow], p.splits) : 0;   // (tokens of no request have none)
-    }
+    int4 info{0, 0, 0, 0};
+    if (orow < rows) info = p.info[orow];
+    const int used = orow < rows && orow / a.Hq < a.cu[a.B] ? min(info.x, kMaxParts) : 0;   // (tokens of no request have none)
     if (used <= 1 && kLanes > 64) return;                    // (all of a workgroup; otherwise it has a barrier to reach)
+    const int64_t first = info.y, stride = info.z;
     // maximum and sum (every wavefront of the row by itself), and the parts' weights
+    f2 mine[kEach];
     float top = -INFINITY, sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < (kParts < 64 ? 1 : kParts / 64); ++i) {
-        if (lane + 64 * i >= used) mine[i] = f2{-INFINITY, 0.f};
-        top = fmaxf(top, mine[i][0]);
+    for (int i = 0; i < kEach; ++i) {
+        mine[i] = f2{-INFINITY, 0.f};
+        if (lane + 64 * i < used) mine[i] = reinterpret_cast<const f2 *>(p.part_ml)[first + (lane + 64 * i) * stride];
     }
+    const int lanes = D / 4, parts = kLanes / lanes, s0 = tid / lanes, d = 4 * (tid % lanes);
+    float4 e[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (s0 < parts && s0 + i * parts < used) e[i] = *reinterpret_cast<const float4 *>(p.part + (first + (s0 + i * parts) * stride) * D + d);
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) top = fmaxf(top, mine[i][0]);
 #pragma unroll
     for (int sh = 32; sh >= 1; sh >>= 1) top = fmaxf(top, __shfl_xor(top, sh));
 #pragma unroll
-    for (int i = 0; i < (kParts < 64 ? 1 : kParts / 64); ++i) {
+    for (int i = 0; i < kEach; ++i) {
         const float w = mine[i][0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mine[i][0] - top);
         if (w != 0.f) sum += w * mine[i][1];
-        if (lane + 64 * i < kParts) w_sh[group][lane + 64 * i] = w;     // (the same from every wavefront of the row)
+        if (lane + 64 * i < used) w_sh[group][lane + 64 * i] = w;       // (the same from every wavefront of the row)
     }
 #pragma unroll
     for (int sh = 32; sh >= 1; sh >>= 1) sum += __shfl_xor(sum, sh);
     __syncthreads();
-    const int lanes = D / 4, parts = kLanes / lanes, s0 = tid / lanes, d = 4 * (tid % lanes);
     float4 v{0.f, 0.f, 0.f, 0.f};
     if (s0 < parts) {
-        const float *src = p.part + orow * D + d;
         for (int s1 = s0; s1 < used; s1 += 8 * parts) {
-            float4 e[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-                if (s1 + i * parts < used) e[i] = *reinterpret_cast<const float4 *>(src + (int64_t)(s1 + i * parts) * rows * D);
+                if (s1 > s0 && s1 + i * parts < used) e[i] = *reinterpret_cast<const float4 *>(p.part + (first + (s1 + i * parts) * stride) * D + d);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float w = s1 + i * parts < used ? w_sh[group][s1 + i * parts] : 0.f;
@@ -594,8 +753,8 @@ template <typename T, int kLanes> __global__ void __launch_bounds__(256) sd_join
     __syncthreads();
     if (used > 1 && tid < lanes) {
         for (int s = 1; s < parts; ++s) {
-            const float4 e = v_sh[group][s * lanes + tid];
-            v.x += e.x; v.y += e.y; v.z += e.z; v.w += e.w;
+            const float4 o = v_sh[group][s * lanes + tid];
+            v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w;
         }
         const float inv = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;
         const int64_t t = orow / a.Hq, head = orow % a.Hq;
@@ -626,34 +785,51 @@ int check(const sd_attention &a)
     return SD_OK;
 }
 
-// ---- which kernel, and how many splits: by the shapes alone ----
-struct Plan { int dk, rows, tiles, splits, min_steps, order; };   // rows of a tile
+// ---- which kernel, and how many workgroups: by the shapes alone ----
+struct Plan { int dk, rows, tiles, splits, min_steps, units, once, pairs; bool level, join; };
 Plan plan_of(const sd_attention &a)
 {
     Plan p;
-    const int64_t G = a.Hq / a.cache.heads, D = a.cache.D, rows = a.tokens * G;
+    const int64_t heads = a.cache.heads, G = a.Hq / heads, D = a.cache.D, rows = a.tokens * G;
     p.dk = D <= 64 ? 64 : D <= 96 ? 96 : D <= 128 ? 128 : D <= 192 ? 192 : 256;
+    // From one and a half tiles of 32 rows a request on, four wavefronts of rows share the keys; below, wavefronts take keys of their own.
     const bool many = rows > 48 * a.B;
     p.rows = many ? 128 : 32;
-    p.tiles = (int)(rows / p.rows + a.B) | 1;              // (odd: the splits of a tile go to different dies)
     const int64_t step = many ? (p.dk <= 128 ? 64 : 32) : (p.dk <= 128 ? 2 : 1) * 32;   // keys
-    // enough workgroups for the chip, as far as the longest context allows
-    const int64_t there = (rows / p.rows > a.B ? rows / p.rows : a.B) * a.cache.heads;
+    const int64_t there = (rows / p.rows > a.B ? rows / p.rows : a.B) * heads;          // workgroups, nothing split
     int64_t longest = a.width * a.cache.page;
     if (a.window > 0 && a.window + p.rows / G + 1 < longest) longest = a.window + p.rows / G + 1;
-    int64_t splits = there < 256 || !many ? (512 + there - 1) / there : 1;
     p.min_steps = there >= 256 ? 16 : there >= 64 ? 4 : 2;
-    const int64_t most = (longest + p.min_steps * step - 1) / (p.min_steps * step);
-    if (splits > most) splits = most;
-    if (splits > 256) splits = 256;
-    p.splits = (int)(splits < 1 ? 1 : splits);
-    // Requests of one part each are of any length.  Where all workgroups find room at once, two to a compute unit (the i-th and the i + 256-th), a long
-    // one next to a short one (64 x 5 tokens over 200 - 4096 keys: 122 us, as they come 135, longest first 136).
-    p.order = many || p.splits > 1 || a.B > 64 || a.B * a.cache.heads > 512 ? 0 : (int)((256 + a.cache.heads - 1) / a.cache.heads);
+    const int64_t most = (longest + p.min_steps * step - 1) / (p.min_steps * step);     // parts of the longest context
+    p.tiles = (int)(rows / p.rows + a.B);
+    p.splits = 1;
+    p.units = p.once = p.pairs = 0;
+    p.level = false;
+    if (many) {
+        // a compute unit has room for two workgroups: where they do not fill the chip once, the keys are split
+        int64_t splits = there < 256 ? (512 + there - 1) / there : 1;
+        splits = splits > most ? most : splits;
+        p.splits = (int)(splits > 256 ? 256 : splits < 1 ? 1 : splits);
+        p.join = p.splits > 1;
+        return p;
+    }
+    // Decoding: where the requests alone do not fill the chip, parts of one length, as many as find room at once.  Contexts far beyond the mean are split in
+    // any case, if the tables are wide enough for such that a workgroup would be long at it (8192 keys of D = 128 take about 170 us).
+    const int64_t once = (512 + heads - 1) / heads < (int64_t)p.tiles * most ? (512 + heads - 1) / heads : (int64_t)p.tiles * most;
+    p.once = there < 512 && most > 1 ? (int)once : 0;
+    p.level = longest * D > 8192 * 128;
+    const int64_t room = p.tiles + (a.B / 2 > 8 ? a.B / 2 : 8), units = p.level && room > p.once ? room : p.once > p.tiles ? p.once : p.tiles;
+    if (units * heads * 32 > 0x7fffffff) { p.once = 0; p.level = false; }            // (rows of parts are numbered in 32 bits)
+    p.units = p.once || p.level ? (int)units : p.tiles;
+    // A compute unit gets the i-th and the i + 256-th workgroup: a long request next to a short one (64 x 5 tokens over 200 - 4096 keys: 122 us; as they
+    // come 135, longest first 136).
+    p.pairs = there >= 256 ? (int)((256 + heads - 1) / heads) : 0;
+    p.join = p.once || p.level;
     return p;
 }
-// parts, (maximum, sum) of each, and the number of parts of a row
-size_t part_bytes(const sd_attention &a, const Plan &p) { return p.splits > 1 ? (size_t)a.tokens * a.Hq * ((size_t)p.splits * (a.cache.D + 2) + 1) * 4 : 0; }
+int64_t part_rows(const sd_attention &a, const Plan &p) { return p.rows == 128 ? (int64_t)p.splits * a.tokens * a.Hq : (int64_t)p.units * a.cache.heads * 32; }
+// parts, (maximum, sum) of each, and where a row's parts are
+size_t part_bytes(const sd_attention &a, const Plan &p) { return p.join ? (size_t)part_rows(a, p) * (a.cache.D + 2) * 4 + (size_t)a.tokens * a.Hq * sizeof(int4) : 0; }
 
 template <typename T, int DK, bool kFull, int kRows, int kKeys, int KT> void launch_shape(const Attend &p, dim3 grid, hipStream_t st)
 {
@@ -666,14 +842,13 @@ template <typename T, int DK, bool kFull, int kRows, int kKeys, int KT> void lau
 }
 template <typename T, int DK, bool kFull> void launch(const Attend &p, const Plan &plan, hipStream_t st)
 {
-    const int64_t items = (int64_t)plan.tiles * plan.splits;
-    const dim3 grid((unsigned)(p.a.cache.heads * (plan.rows == 128 ? items : (items + 7) / 8 * 8)));
+    const dim3 grid((unsigned)(p.a.cache.heads * (plan.rows == 128 ? (int64_t)plan.tiles * plan.splits : ((int64_t)plan.units + 7) / 8 * 8)));
     constexpr int kKeys = DK <= 128 ? 2 : 1, KT = DK <= 128 ? 64 : 32;
     if (plan.rows == 128) launch_shape<T, DK, kFull, 4, 1, KT>(p, grid, st);
     else launch_shape<T, DK, kFull, 1, kKeys, 32>(p, grid, st);
-    if (plan.splits > 1) {
+    if (plan.join) {
         const int64_t rows = p.a.tokens * p.a.Hq;
-        if (plan.splits > 8) hipLaunchKernelGGL((sd_join_kernel<T, 256>), dim3((unsigned)rows), dim3(256), 0, st, p);
+        if (rows <= 1024) hipLaunchKernelGGL((sd_join_kernel<T, 256>), dim3((unsigned)rows), dim3(256), 0, st, p);
         else hipLaunchKernelGGL((sd_join_kernel<T, 64>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, p);
     }
 }
@@ -729,10 +904,14 @@ int sd_attend(const sd_attention *args, void *ws, size_t ws_bytes, void *hip_str
     p.splits = plan.splits;
     p.min_steps = plan.min_steps;
     p.row_tiles = plan.tiles;
-    p.order = plan.order;
-    p.part = static_cast<float *>(ws);
-    p.part_ml = p.part + (size_t)plan.splits * a.tokens * a.Hq * a.cache.D;
-    p.used = reinterpret_cast<int *>(p.part_ml + (size_t)plan.splits * a.tokens * a.Hq * 2);
+    p.units = plan.units;
+    p.once = plan.once;
+    p.level = plan.level;
+    p.pairs = plan.pairs;
+    const size_t parts = (size_t)part_rows(a, plan);
+    p.info = plan.join ? static_cast<int4 *>(ws) : nullptr;
+    p.part = reinterpret_cast<float *>(static_cast<int4 *>(ws) + (size_t)a.tokens * a.Hq);
+    p.part_ml = p.part + parts * a.cache.D;
     if (a.cache.dtype == SD_BF16) launch<__bf16>(p, plan, static_cast<hipStream_t>(hip_stream));
     else launch<_Float16>(p, plan, static_cast<hipStream_t>(hip_stream));
     return hipGetLastError() == hipSuccess ? SD_OK : SD_EHIP;

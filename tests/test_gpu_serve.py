@@ -298,6 +298,32 @@ def test_attention_of_many_requests(Bn, most, Hq):
     _Batch(new, kv, Hq, 1, 64, 16, "f16", seed=Bn).check()
 
 
+@pytest.mark.parametrize("new,kv,Hq,Hkv,D,window", [
+    ([1] * 70, [20000] + [50] * 69, 2, 1, 64, 0), ([1, 0, 2] * 34, [9000 if b == 40 else 30 + b for b in range(102)], 8, 8, 128, 0),
+    ([3, 1, 0, 2], [6000, 5000, 4000, 7], 4, 2, 64, 0), ([9] * 5, [700, 5000, 9, 1300, 2500], 8, 1, 128, 0), ([1] * 20, list(range(100, 6100, 300)), 16, 16, 64, 0),
+    ([2, 2, 2], [9000, 400, 8000], 4, 2, 64, 3000), ([1] * 300, [40] * 299 + [12000], 2, 2, 256, 0)])
+def test_attention_of_contexts_of_very_different_lengths(new, kv, Hq, Hkv, D, window):
+    """Keys are split where few requests would leave the chip empty, and where one is far longer than the others."""
+    print("case", len(new), max(kv), Hq, Hkv, D, flush=True)
+    _Batch(new, kv, Hq, Hkv, D, 16, "bf16", seed=D + len(new), window=window).check()
+
+
+def test_attention_clamps_what_the_host_cannot_see():
+    """Offsets, lengths and page numbers out of range give some result, inside the arrays."""
+    torch = _torch()
+    for new, kv in (([2, 3, 1], [2500, 100, 900]), ([90, 60, 50], [200, 300, 60])):
+        b = _Batch(new, kv, 4, 2, 64, 16, "bf16", seed=5)
+        T = sum(new)
+        for cu, lengths in (([0, T, 0, T], kv), ([-5, 1 << 30, 7, -1], kv), ([0, 0, 0, 0], kv), (b.cu.tolist(), [-1, 1 << 30, 0x7fffffff])):
+            bad = _Batch(new, kv, 4, 2, 64, 16, "bf16", seed=5)
+            bad.cu, bad.kv, bad.table = np.array(cu, np.int32), lengths, np.where(bad.table == 1 << 30, -7, bad.table)
+            out, _ = bad.gpu()
+            assert out.shape[0] == T
+        want, _ = b.gpu()
+        assert torch.isfinite(want).all()                       # and the next call is not the worse for it
+        b.check()
+
+
 def test_attention_of_a_padded_batch():
     """Rows past the last request's are nobody's: they are left alone, the others' are the same."""
     torch = _torch()
