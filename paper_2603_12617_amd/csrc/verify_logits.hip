@@ -106,6 +106,48 @@ __device__ __forceinline__ float power_any(float l, float top, Heat h)
     return d * h.hi >= -125.f ? __builtin_amdgcn_exp2f(__builtin_fmaf(d, h.lo, d * h.hi)) : 0.f;
 }
 
+// ---- reductions by lane moves within the wavefront's registers (a trip through LDS per step would be the larger part of a small call) ----
+// lanes without a source, and rows outside ROWS, get `none`
+template <int CTRL, int ROWS> __device__ __forceinline__ int moved(int v, int none) { return __builtin_amdgcn_update_dpp(none, v, CTRL, ROWS, 0xF, false); }
+template <int CTRL, int ROWS> __device__ __forceinline__ float moved(float v, float none) { return __int_as_float(moved<CTRL, ROWS>(__float_as_int(v), __float_as_int(none))); }
+template <int CTRL, int ROWS> __device__ __forceinline__ double moved(double v, double none)
+{
+    const long long u = __double_as_longlong(v), n = __double_as_longlong(none);
+    const unsigned lo = (unsigned)moved<CTRL, ROWS>((int)u, (int)n), hi = (unsigned)moved<CTRL, ROWS>((int)(u >> 32), (int)(n >> 32));
+    return __longlong_as_double((long long)((u64)hi << 32 | lo));
+}
+// f over the lanes of each half of a wavefront, in its last lane
+template <typename V, typename F> __device__ __forceinline__ V over_half(V v, V none, F f)
+{
+    v = f(v, moved<0x111, 0xF>(v, none));      // row_shr:1
+    v = f(v, moved<0x112, 0xF>(v, none));
+    v = f(v, moved<0x114, 0xF>(v, none));
+    v = f(v, moved<0x118, 0xF>(v, none));
+    return f(v, moved<0x142, 0xA>(v, none));   // row_bcast:15
+}
+// the last lane of this lane's half
+__device__ __forceinline__ int of_half(int v, int lane) { return lane < 32 ? __builtin_amdgcn_readlane(v, 31) : __builtin_amdgcn_readlane(v, 63); }
+__device__ __forceinline__ float of_half(float v, int lane) { return __int_as_float(of_half(__float_as_int(v), lane)); }
+__device__ __forceinline__ double of_half(double v, int lane)
+{
+    const long long u = __double_as_longlong(v);
+    return __longlong_as_double((long long)((u64)(unsigned)of_half((int)(u >> 32), lane) << 32 | (unsigned)of_half((int)u, lane)));
+}
+// f over all lanes
+template <typename F> __device__ __forceinline__ int over_all(int v, int none, F f)
+{
+    v = over_half(v, none, f);
+    return __builtin_amdgcn_readlane(f(v, moved<0x143, 0xC>(v, none)), 63);      // row_bcast:31
+}
+template <typename F> __device__ __forceinline__ float over_all(float v, float none, F f)
+{
+    v = over_half(v, none, f);
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f(v, moved<0x143, 0xC>(v, none))), 63));
+}
+constexpr auto kMax = [](auto a, auto b) { return a > b ? a : b; };
+constexpr auto kMin = [](auto a, auto b) { return a < b ? a : b; };
+constexpr auto kSum = [](auto a, auto b) { return a + b; };
+
 // the request of a row: the last b with cu[b] <= row (target rows) or cu[b] - b <= row (drafts' rows); by the lanes of a wavefront
 __device__ __forceinline__ int request_of(const int32_t *cu, int B, int row, bool draft, int lane)
 {
@@ -145,8 +187,7 @@ __global__ void __launch_bounds__(kThreads) sd_stats_kernel(const sd_logits s, S
     for (int c = 0; c < kC; ++c)
 #pragma unroll
         for (int e = 0; e < E::kVec; ++e) top = fmaxf(top, E::get(raw[c], e));
-#pragma unroll
-    for (int sh = 32; sh >= 1; sh >>= 1) top = fmaxf(top, __shfl_xor(top, sh));
+    top = over_all(top, kNone, kMax);
     if (lane == 0) top_sh[wave] = top;
     __syncthreads();
 #pragma unroll
@@ -180,8 +221,7 @@ __global__ void __launch_bounds__(kThreads) sd_stats_kernel(const sd_logits s, S
             for (int e = E::kVec - 1; e >= 0; --e)
                 if (E::get(raw[c], e) == top) at = place<T>(seg, c) + e;
     }
-#pragma unroll
-    for (int sh = 32; sh >= 1; sh >>= 1) { at = min(at, __shfl_xor(at, sh)); sum += __shfl_xor(sum, sh); }
+    if (hot) sum = over_all(sum, 0.f, kSum); else at = over_all(at, 0x7fffffff, kMin);
     if (lane == 0) { at_sh[wave] = at; sum_sh[wave] = sum; }
     __syncthreads();
     if (tid == 0) {
@@ -195,23 +235,22 @@ __global__ void __launch_bounds__(kThreads) sd_stats_kernel(const sd_logits s, S
 
 // A row's parts joined by the 32 lanes of half a wavefront, in a fixed order; each of them gets the result.
 struct Row { float top, inv; int best; };      // inv: 1 / the sum of the weights, 0 without a finite logit
-__device__ __forceinline__ Row join(const Stat *stat, int segs, Heat h, int lane)
+__device__ __forceinline__ Stat part(const Stat *stat, int segs, int lane)
 {
     const int s = lane & 31;
-    Stat r{kNone, 0.f, 0x7fffffff};
-    if (s < segs) r = stat[s];
-    float top = r.top;
-#pragma unroll
-    for (int sh = 16; sh >= 1; sh >>= 1) top = fmaxf(top, __shfl_xor(top, sh));
-    int best = r.top == top ? r.at : 0x7fffffff;
+    return s < segs ? stat[s] : Stat{kNone, 0.f, 0x7fffffff};
+}
+__device__ __forceinline__ Row join(const Stat &r, Heat h, int lane)
+{
+    const float top = of_half(over_half(r.top, kNone, kMax), lane);
+    const int best = of_half(over_half(r.top == top ? r.at : 0x7fffffff, 0x7fffffff, kMin), lane);
     // (sums are relative to top c rounded to float where that is tame)
     double sum = 0.0;
     if (r.top > kNone) {
         const float back = tame(top, h) && tame(r.top, h) ? exp2f((float)((double)(r.top * h.hi) - (double)(top * h.hi))) : power_any(r.top, top, h);
         sum = (double)r.sum * (double)back;
     }
-#pragma unroll
-    for (int sh = 16; sh >= 1; sh >>= 1) { best = min(best, __shfl_xor(best, sh)); sum += __shfl_xor(sum, sh); }
+    sum = of_half(over_half(sum, 0.0, kSum), lane);
     Row w;
     w.top = top;
     w.best = top > kNone ? best : 0;
@@ -229,12 +268,12 @@ __device__ __forceinline__ float weight(float l, const Row &r, Heat h)
 __device__ __forceinline__ u64 entry(float score, int x) { return ((u64)__float_as_uint(score) << 32) | (0xffffffffu - (unsigned)x); }
 __device__ __forceinline__ u64 larger(u64 a, u64 b) { return a > b ? a : b; }
 
-// the largest entry of a workgroup, for thread 0
-__device__ __forceinline__ u64 first_of(u64 v, u64 *sh)
+// the entry of a workgroup's best score, which is positive or 0 for none
+__device__ __forceinline__ u64 first_of(float score, int x, u64 *sh)
 {
-#pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) v = larger(v, __shfl_xor(v, d));
-    if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
+    const float best = over_all(score, 0.f, kMax);
+    const int at = over_all(score == best ? x : 0x7fffffff, 0x7fffffff, kMin);
+    if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = best > 0.f ? entry(best, at) : 0;
     __syncthreads();
     return larger(larger(sh[0], sh[1]), larger(sh[2], sh[3]));
 }
@@ -281,9 +320,10 @@ __global__ void __launch_bounds__(kThreads) sd_draw_kernel(const sd_logits s, co
                     if (Q) ql = one(Q + (int64_t)(first + j) * s.q_stride + x);
                 }
             }
-            const Row p = join(stat + (int64_t)(row0 + j) * segs, segs, h, lane);
+            const Stat ps = part(stat + (int64_t)(row0 + j) * segs, segs, lane), qs = Q && j < k ? part(stat + (int64_t)(rows + first + j) * segs, segs, lane) : ps;
+            const Row p = join(ps, h, lane);
             Row q{0.f, 0.f, 0};
-            if (Q && j < k) q = join(stat + (int64_t)(rows + first + j) * segs, segs, h, lane);
+            if (Q && j < k) q = join(qs, h, lane);
             if ((tid & 31) == 0) {
                 if (j < kKeep) { row_sh[0][j] = p; row_sh[1][j] = q; }
                 if (j < k && !(hot ? __fmul_rn(r, Q ? weight(ql, q, h) : 1.f) <= weight(pl, p, h) : x == p.best)) atomicMin(&n_sh, j);
@@ -298,8 +338,8 @@ __global__ void __launch_bounds__(kThreads) sd_draw_kernel(const sd_logits s, co
     Row p, q{0.f, 0.f, 0};
     if (n < kKeep) { p = row_sh[0][n]; q = row_sh[1][n]; }
     else {
-        p = join(stat + (int64_t)(row0 + n) * segs, segs, h, lane);
-        if (Q && rejected) q = join(stat + (int64_t)(rows + first + n) * segs, segs, h, lane);
+        p = join(part(stat + (int64_t)(row0 + n) * segs, segs, lane), h, lane);
+        if (Q && rejected) q = join(part(stat + (int64_t)(rows + first + n) * segs, segs, lane), h, lane);
     }
     if (!hot || p.top == kNone) {
         if (seg == 0 && tid == 0) { n_out[b] = n; next_out[b] = p.top == kNone ? 0 : p.best; }
@@ -344,7 +384,7 @@ __global__ void __launch_bounds__(kThreads) sd_draw_kernel(const sd_logits s, co
                 if (sc > won) { won = sc; at = c * E::kVec + i; }
             }
     }
-    u64 best = first_of(won > 0.f ? entry(won, place<T>(seg, at / E::kVec) + at % E::kVec) : 0, best_sh);
+    u64 best = first_of(won, place<T>(seg, at / E::kVec) + at % E::kVec, best_sh);
     if (tid == 0) {
         bool last = true;
         if (segs > 1) {
@@ -369,7 +409,7 @@ __global__ void __launch_bounds__(kThreads) sd_draw_kernel(const sd_logits s, co
         const float sc = weight(one(prow + x), p, h) * __builtin_amdgcn_rcpf(noise[x]);
         if (sc > won) { won = sc; x_won = x; }
     }
-    best = first_of(won > 0.f ? entry(won, x_won) : 0, best_sh);
+    best = first_of(won, x_won, best_sh);
     if (tid == 0) { n_out[b] = n; next_out[b] = best ? (int)(0xffffffffu - (unsigned)best) : 0; }
 }
 
