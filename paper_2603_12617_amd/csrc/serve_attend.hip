@@ -103,6 +103,7 @@ struct Attend {
     float scale;                   // scale * log2(e): weights are powers of two
     int splits, min_steps;         // chunks: parts that a tile's keys are split into at most; steps of keys that a part has at least
     int row_tiles;                 // chunks: tiles of rows there may be
+    bool grouped;                  // chunks: an eighth of the heads to each die
     int units, once;               // decoding: workgroups of a key head; so many of them find room at once (0: they are not split to fill it)
     bool level;                    // decoding: what is far longer than the others is split
     int pairs;                     // decoding: where all workgroups find room at once, so many come longest first, the others shortest first (0: as they come)
@@ -365,11 +366,24 @@ __global__ void __launch_bounds__(64 * kRows * kKeys, DK > 192 || (kRows == 1 &&
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = kRows > 1 ? wave : 0, wk = kRows > 1 ? 0 : wave;
     const int half = lane >> 5, col = lane & 31;
-    // The chip deals workgroups to its eight dies in turn.  Chunks: a key head's tiles of rows go to one die (of eight heads), whose cache then holds
-    // its keys.  Decoding, where keys are read once: the heads of a range of keys one after the other on one die, so that the pieces of a token's
-    // row are fetched at about the same time.
-    const unsigned heads = (unsigned)a.cache.heads, turn = kOwn ? blockIdx.x / 8 : blockIdx.x, item = kOwn ? turn / heads * 8 + blockIdx.x % 8 : turn / heads;
-    const int kh = turn % heads;
+    // The chip deals workgroups to its eight dies in turn.  Chunks, grouped: an eighth of the key heads, neighbours, to each die, whose cache then holds their
+    // keys for all tiles of a request, and the lines of memory that neighbouring heads share; where the heads are no multiple of eight, the borders move
+    // from tile to tile.  Otherwise in turn.  Decoding, where keys are read once: the heads of a range of keys one after the other on one die, so
+    // that the pieces of a token's row are fetched at about the same time.
+    const unsigned heads = (unsigned)a.cache.heads, die = blockIdx.x % 8, turn = blockIdx.x / 8;
+    unsigned item;
+    int kh;
+    if (kOwn) {
+        item = turn / heads * 8 + die;
+        kh = turn % heads;
+    } else if (!p.grouped) {
+        item = blockIdx.x / heads;
+        kh = blockIdx.x % heads;
+    } else {
+        const unsigned each = (heads + 7) / 8, shift = 7 - (item = turn / each) % 8;     // (head h is on die (8 h + 7 - shift) / heads)
+        kh = (die * heads + shift) / 8 + turn % each;
+        if (kh >= (int)(((die + 1) * heads + shift) / 8)) return;
+    }
     const int D = kFull ? DK : (int)a.cache.D, G = p.G, page = (int)a.cache.page;
 
     int b, row0, t0, t1, parts, part_row = 0, part_step = 0, split;      // tiles of keys t0, t0 + kKeys, .. < t1; where the parts of row 0 lie, by rows
@@ -786,7 +800,7 @@ int check(const sd_attention &a)
 }
 
 // ---- which kernel, and how many workgroups: by the shapes alone ----
-struct Plan { int dk, rows, tiles, splits, min_steps, units, once, pairs; bool level, join; };
+struct Plan { int dk, rows, tiles, splits, min_steps, units, once, pairs; bool level, join, grouped; };
 Plan plan_of(const sd_attention &a)
 {
     Plan p;
@@ -804,13 +818,17 @@ Plan plan_of(const sd_attention &a)
     p.tiles = (int)(rows / p.rows + a.B);
     p.splits = 1;
     p.units = p.once = p.pairs = 0;
-    p.level = false;
+    p.level = p.grouped = false;
     if (many) {
         // a compute unit has room for two workgroups: where they do not fill the chip once, the keys are split
         int64_t splits = there < 256 ? (512 + there - 1) / there : 1;
         splits = splits > most ? most : splits;
         p.splits = (int)(splits > 256 ? 256 : splits < 1 ? 1 : splits);
         p.join = p.splits > 1;
+        // Neighbouring heads share lines of memory where a head's piece is no multiple of 128 bytes (20 heads, 24 chunks of 150 tokens over 1500 keys, D = 96:
+        // 144 us in turn, 99 grouped); where it is, the places that 20 heads leave empty cost more than the keys shared by a request's tiles bring (25
+        // chunks of 128, D = 64: 35 and 44).
+        p.grouped = heads > 8 && (heads % 8 == 0 || (D % 64 != 0 && a.cache.k_head_stride < a.cache.k_tok_stride));
         return p;
     }
     // Decoding: where the requests alone do not fill the chip, parts of one length, as many as find room at once.  Contexts far beyond the mean are split in
@@ -842,7 +860,8 @@ template <typename T, int DK, bool kFull, int kRows, int kKeys, int KT> void lau
 }
 template <typename T, int DK, bool kFull> void launch(const Attend &p, const Plan &plan, hipStream_t st)
 {
-    const dim3 grid((unsigned)(p.a.cache.heads * (plan.rows == 128 ? (int64_t)plan.tiles * plan.splits : ((int64_t)plan.units + 7) / 8 * 8)));
+    const int64_t heads = p.a.cache.heads, items = (int64_t)plan.tiles * plan.splits;
+    const dim3 grid((unsigned)(plan.rows == 32 ? ((int64_t)plan.units + 7) / 8 * 8 * heads : plan.grouped ? items * ((heads + 7) / 8 * 8) : items * heads));
     constexpr int kKeys = DK <= 128 ? 2 : 1, KT = DK <= 128 ? 64 : 32;
     if (plan.rows == 128) launch_shape<T, DK, kFull, 4, 1, KT>(p, grid, st);
     else launch_shape<T, DK, kFull, 1, kKeys, 32>(p, grid, st);
@@ -904,6 +923,7 @@ int sd_attend(const sd_attention *args, void *ws, size_t ws_bytes, void *hip_str
     p.splits = plan.splits;
     p.min_steps = plan.min_steps;
     p.row_tiles = plan.tiles;
+    p.grouped = plan.grouped;
     p.units = plan.units;
     p.once = plan.once;
     p.level = plan.level;
