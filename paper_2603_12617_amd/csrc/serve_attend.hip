@@ -353,6 +353,7 @@ template <typename T, int DK, bool kFull, int kRows, int kKeys, int KT>
 __global__ void __launch_bounds__(64 * kRows * kKeys, DK > 192 || (kRows == 1 && DK > 128) ? 1 : 2) sd_attend_kernel(const Attend p)
 {
     static_assert(kRows == 1 || kKeys == 1, "wavefronts differ in rows or in keys");
+    static_assert(!kFull || 2 * DK == Shape<DK>::kPitch, "loads without a test take every piece of a row of LDS, so each has to be one of the head's");
     constexpr bool kOwn = kRows == 1;                        // a wavefront has keys of its own
     typedef Shape<DK> S;
     constexpr int kTile = KT * S::kPitch;                    // bytes of a tile of keys or values
@@ -873,8 +874,11 @@ template <typename T, int DK, bool kFull> void launch(const Attend &p, const Pla
 }
 template <typename T, int DK> void launch(const Attend &p, const Plan &plan, hipStream_t st)
 {
-    if (p.a.cache.D == DK) launch<T, DK, true>(p, plan, st);
-    else launch<T, DK, false>(p, plan, st);
+    // (a head of 96 or 192 fills its row of products, but not the 128 or 256 elements from row to row in LDS)
+    if constexpr (2 * DK == Shape<DK>::kPitch) {
+        if (p.a.cache.D == DK) { launch<T, DK, true>(p, plan, st); return; }
+    }
+    launch<T, DK, false>(p, plan, st);
 }
 template <typename T> void launch(const Attend &p, const Plan &plan, hipStream_t st)
 {

@@ -363,6 +363,16 @@ def test_attention_offsets_beyond_32_bits():
     assert torch.equal(out, out2) and float(out.float().abs().sum()) > 0
 
 
+@pytest.mark.parametrize("D", [96, 192, 128])
+@pytest.mark.parametrize("new", [[5, 1], [200, 40]])
+def test_attention_reads_nothing_behind_the_cache(D, new):
+    """A cache that ends where its memory does (whole blocks of 2 MiB), its last row in use: heads that do not fill their row of LDS too."""
+    b = _Batch(new, [64 * 127, 64], 8, 8, D, 64, "bf16", seed=D, spare=0)
+    assert b.k.numel() * 2 % (2 << 20) == 0 and b.k.shape[0] - 1 in b.table[:, :127]
+    print("case", D, new, flush=True)
+    b.check()
+
+
 def test_attention_repeats_its_bits_and_runs_on_other_streams():
     torch = _torch()
     b = _Batch([5, 33, 1], [900, 400, 2000], 8, 2, 128, 16, "bf16", seed=12)
