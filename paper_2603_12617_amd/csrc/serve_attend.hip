@@ -108,6 +108,7 @@ struct Attend {
     bool level;                    // decoding: what is far longer than the others is split
     int pairs;                     // decoding: where all workgroups find room at once, so many come longest first, the others shortest first (0: as they come)
     float *part, *part_ml;         // [.][D], [.][2]: weighted values, (maximum, sum) of a row's part
+    int64_t part_rows;             // rows of parts there are
     int4 *info;                    // [tokens * Hq]: how many parts a row has, where its first is, how far apart they are
 };
 
@@ -722,9 +723,12 @@ template <typename T, int kLanes> __global__ void __launch_bounds__(256) sd_join
     const int D = (int)a.cache.D;
     int4 info{0, 0, 0, 0};
     if (orow < rows) info = p.info[orow];
-    const int used = orow < rows && orow / a.Hq < a.cu[a.B] ? min(info.x, kMaxParts) : 0;   // (tokens of no request have none)
+    const int64_t first = info.y, stride = info.z, token = orow / a.Hq;
+    // Tokens of no request have no parts, only what the workspace held; row offsets that do not ascend may leave such tokens between requests, too.
+    const bool of_one = orow < rows && token >= a.cu[0] && token < a.cu[a.B] && info.x > 1 && info.x <= kMaxParts && first >= 0 && stride >= 0 &&
+                        first + (info.x - 1) * stride < p.part_rows;
+    const int used = of_one ? info.x : 0;
     if (used <= 1 && kLanes > 64) return;                    // (all of a workgroup; otherwise it has a barrier to reach)
-    const int64_t first = info.y, stride = info.z;
     // maximum and sum (every wavefront of the row by itself), and the parts' weights
     f2 mine[kEach];
     float top = -INFINITY, sum = 0.f;
@@ -933,6 +937,7 @@ int sd_attend(const sd_attention *args, void *ws, size_t ws_bytes, void *hip_str
     p.level = plan.level;
     p.pairs = plan.pairs;
     const size_t parts = (size_t)part_rows(a, plan);
+    p.part_rows = plan.join ? (int64_t)parts : 0;
     p.info = plan.join ? static_cast<int4 *>(ws) : nullptr;
     p.part = reinterpret_cast<float *>(static_cast<int4 *>(ws) + (size_t)a.tokens * a.Hq);
     p.part_ml = p.part + parts * a.cache.D;

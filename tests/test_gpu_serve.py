@@ -324,6 +324,30 @@ def test_attention_clamps_what_the_host_cannot_see():
         b.check()
 
 
+def test_attention_workspace_contents_do_not_matter():
+    """Tokens before the first request's have no parts: whatever the workspace holds in their place is not taken for some."""
+    torch = _torch()
+    for new, kv in (([2, 3], [2500, 100]), ([90, 60], [200, 300])):
+        b = _Batch(new, kv, 4, 2, 64, 16, "bf16", seed=5)
+        want, _ = b.gpu()
+        q, k, v = (x.to(DEV) for x in (b.q, b.k, b.v))
+        cu, lengths, table = _i32(b.cu), _i32(b.kv), _i32(b.table)
+        cu[0] = 1                                                # (the first request has a token less; its others stand where they did)
+        for fill in (0x7f, 0x00, 0x01, 0x80, 0xff):
+            out = torch.full(tuple(q.shape), -7.0, dtype=q.dtype, device=DEV)
+            ws = torch.full((B.sd_attend_workspace_bytes(q, k, table),), fill, dtype=torch.uint8, device=DEV)
+            for _ in range(2):                                   # (and what the last call left there)
+                B.sd_attend(q, k, v, cu, lengths, table, out, b.scale, ws=ws)
+            torch.cuda.synchronize()
+            assert (out[0] == -7).all() and (out[1:] != -7).any(dim=-1).all()
+            B.sd_attend(q, k, v, _i32(b.cu), lengths, table, out, b.scale, ws=ws)
+            torch.cuda.synchronize()
+            assert torch.equal(out, want)
+            B.sd_attend(q, k, v, cu, lengths, table, out.fill_(-7.0), b.scale, ws=ws)     # (row 0's parts lie there now)
+            torch.cuda.synchronize()
+            assert (out[0] == -7).all()
+
+
 def test_attention_of_a_padded_batch():
     """Rows past the last request's are nobody's: they are left alone, the others' are the same."""
     torch = _torch()
