@@ -3,8 +3,8 @@
 //   stats   every row of V logits in segments of kSeg, a workgroup each: the largest logit and, of the rows of requests with a
 //           temperature, sum 2^(l c - top c), c = log2(e) / tau, of greedy ones the largest's first place.  All segments are independent,
 //           so a batch of one request fills V / kSeg workgroups a row and a large one the chip; each logit is read once.
-//   draw    per request and segment: the rows' partial sums are joined (again by every workgroup of the request: a few
-//           hundred numbers from L2, in a fixed order, half a wavefront to a row), the drafts tested, and the segment of row n
+//   draw    per request and kRace places: the rows' partial sums are joined (again by every workgroup of the request: a few
+//           hundred numbers from L2, in a fixed order, half a wavefront to a row), the drafts tested, and these places of row n
 //           raced: score(x) = weight(x) / noise(x).  Workgroups of a request meet in a 64-bit maximum of
 //           (score's bits, lowest place), whose order does not matter; the last one writes n and next.
 //
@@ -25,6 +25,11 @@ typedef unsigned long long u64;
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kPer = 32;                       // logits of a thread
 constexpr int kSeg = kThreads * kPer;          // of a workgroup
+// Places of a thread of the draw: half as many as a segment has, so that a few requests spread over twice the workgroups (8, 16, 32 of them, us a
+// call: 8 requests of 4 drafts, V = 32000, float: 11.9, 12.2, 13.1; 256 of 4, V = 151936, bfloat16: 208, 189.6, 188.4; 100 of up to 8 without
+// a distribution, V = 50257, float16: 24.1, 22.8, 23.8).
+constexpr int kRacePer = 16;
+constexpr int kRace = kThreads * kRacePer;
 constexpr int kMaxSegs = (SD_MAX_V + kSeg - 1) / kSeg;
 constexpr float kNone = -__builtin_inff();
 static_assert(kMaxSegs <= 32, "half a wavefront joins a row");
@@ -79,8 +84,8 @@ template <typename T> __device__ __forceinline__ typename Vec<T>::Raw load(const
     }
     return v;
 }
-// a thread's logits of segment `seg`: raw[c] from place place(seg, c) on
-template <typename T> __device__ __forceinline__ int place(int seg, int c) { return seg * kSeg + (c * kThreads + (int)threadIdx.x) * Vec<T>::kVec; }
+// a thread's logits of segment `seg` of `size`: raw[c] from place place(seg, c) on
+template <typename T, int size> __device__ __forceinline__ int place(int seg, int c) { return seg * size + (c * kThreads + (int)threadIdx.x) * Vec<T>::kVec; }
 
 // NaN counts as -inf, +inf as the largest float
 __device__ __forceinline__ float clean(float l) { return l == l ? fminf(l, 3.4028234663852886e38f) : kNone; }
@@ -178,7 +183,7 @@ __global__ void __launch_bounds__(kThreads) sd_stats_kernel(const sd_logits s, S
     const T *l = draft ? static_cast<const T *>(s.q) + (int64_t)(row - rows) * s.q_stride : static_cast<const T *>(s.p) + (int64_t)row * s.p_stride;
     typename E::Raw raw[kC];
 #pragma unroll
-    for (int c = 0; c < kC; ++c) raw[c] = load(l, place<T>(seg, c), V);
+    for (int c = 0; c < kC; ++c) raw[c] = load(l, place<T, kSeg>(seg, c), V);
     const float tau = s.tau[request_of(s.cu, B, draft ? row - rows : row, draft, lane)];
     const bool hot = tau > 0.f;
     const Heat h = heat(hot ? tau : 1.f);
@@ -219,7 +224,7 @@ __global__ void __launch_bounds__(kThreads) sd_stats_kernel(const sd_logits s, S
         for (int c = kC - 1; c >= 0; --c)
 #pragma unroll
             for (int e = E::kVec - 1; e >= 0; --e)
-                if (E::get(raw[c], e) == top) at = place<T>(seg, c) + e;
+                if (E::get(raw[c], e) == top) at = place<T, kSeg>(seg, c) + e;
     }
     if (hot) sum = over_all(sum, 0.f, kSum); else at = over_all(at, 0x7fffffff, kMin);
     if (lane == 0) { at_sh[wave] = at; sum_sh[wave] = sum; }
@@ -282,7 +287,7 @@ template <typename T>
 __global__ void __launch_bounds__(kThreads) sd_draw_kernel(const sd_logits s, const Stat *stat, Race *race, int segs, int32_t *n_out, int32_t *next_out)
 {
     typedef Vec<T> E;
-    constexpr int kC = kPer / E::kVec;
+    constexpr int kC = kRacePer / E::kVec;
     constexpr int kKeep = SD_MAX_K + 1;                     // rows whose parts are kept joined; further ones are joined again
     __shared__ Row row_sh[2][kKeep];
     __shared__ int n_sh, last_sh;
@@ -302,7 +307,7 @@ __global__ void __launch_bounds__(kThreads) sd_draw_kernel(const sd_logits s, co
 #pragma unroll
         for (int c = 0; c < kC; ++c)
 #pragma unroll
-            for (int i = 0; i < E::kVec / 4; ++i) e[c * (E::kVec / 4) + i] = load(noise, place<T>(seg, c) + 4 * i, V);
+            for (int i = 0; i < E::kVec / 4; ++i) e[c * (E::kVec / 4) + i] = load(noise, place<T, kRace>(seg, c) + 4 * i, V);
     }
     if (tid == 0) n_sh = k;
     __syncthreads();
@@ -348,10 +353,10 @@ __global__ void __launch_bounds__(kThreads) sd_draw_kernel(const sd_logits s, co
     const T *prow = P + (int64_t)(row0 + n) * s.p_stride, *qrow = Q && rejected ? Q + (int64_t)(first + n) * s.q_stride : nullptr;
     typename E::Raw f[kC], g[kC];
 #pragma unroll
-    for (int c = 0; c < kC; ++c) f[c] = load(prow, place<T>(seg, c), V);
+    for (int c = 0; c < kC; ++c) f[c] = load(prow, place<T, kRace>(seg, c), V);
     if (qrow) {
 #pragma unroll
-        for (int c = 0; c < kC; ++c) g[c] = load(qrow, place<T>(seg, c), V);
+        for (int c = 0; c < kC; ++c) g[c] = load(qrow, place<T, kRace>(seg, c), V);
     } else {
 #pragma unroll
         for (int c = 0; c < kC; ++c) g[c] = E::none();
@@ -368,7 +373,7 @@ __global__ void __launch_bounds__(kThreads) sd_draw_kernel(const sd_logits s, co
                 float w = power(E::get(f[c], i), pref, h) * p.inv;
                 // (the maximum takes what is no number for 0; q.inv = 0 without a rejected draft's row)
                 if (qrow) w = __builtin_fmaf(fmaxf(power(E::get(g[c], i), qref, h), 0.f), -q.inv, w);
-                else if (drafted == place<T>(seg, c) + i) w = 0.f;
+                else if (drafted == place<T, kRace>(seg, c) + i) w = 0.f;
                 const float sc = w * __builtin_amdgcn_rcpf(e[(c * E::kVec + i) / 4][i % 4]);
                 if (sc > won) { won = sc; at = c * E::kVec + i; }     // (places ascend within a thread: of equal scores the first stays)
             }
@@ -379,22 +384,22 @@ __global__ void __launch_bounds__(kThreads) sd_draw_kernel(const sd_logits s, co
             for (int i = 0; i < E::kVec; ++i) {
                 float w = weight(E::get(f[c], i), p, h);
                 if (qrow) w -= weight(E::get(g[c], i), q, h);
-                else if (drafted == place<T>(seg, c) + i) w = 0.f;
+                else if (drafted == place<T, kRace>(seg, c) + i) w = 0.f;
                 const float sc = w * __builtin_amdgcn_rcpf(e[(c * E::kVec + i) / 4][i % 4]);
                 if (sc > won) { won = sc; at = c * E::kVec + i; }
             }
     }
-    u64 best = first_of(won, place<T>(seg, at / E::kVec) + at % E::kVec, best_sh);
+    u64 best = first_of(won, place<T, kRace>(seg, at / E::kVec) + at % E::kVec, best_sh);
     if (tid == 0) {
         bool last = true;
-        if (segs > 1) {
+        if (gridDim.y > 1) {
             // Only atomics carry data between the workgroups, each done (its old value is back) before the next is issued: a fence,
             // which would write back and drop caches, is not needed for that.
             if (best) {
                 u64 old = __hip_atomic_fetch_max(&race[b].best, best, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
                 asm volatile("s_waitcnt vmcnt(0)" : "+v"(old)::"memory");
             }
-            last = __hip_atomic_fetch_add(&race[b].met, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (unsigned)segs - 1;
+            last = __hip_atomic_fetch_add(&race[b].met, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == gridDim.y - 1;
             if (last) best = __hip_atomic_fetch_max(&race[b].best, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         }
         if (last && (best || !rejected)) { n_out[b] = n; next_out[b] = best ? (int)(0xffffffffu - (unsigned)best) : 0; }
@@ -431,7 +436,7 @@ template <typename T> void launch(const sd_logits &s, Stat *stat, Race *race, in
 {
     const unsigned segs = (unsigned)segments(s);
     hipLaunchKernelGGL(sd_stats_kernel<T>, dim3((unsigned)stat_rows(s), segs), dim3(kThreads), 0, st, s, stat, race);
-    hipLaunchKernelGGL(sd_draw_kernel<T>, dim3((unsigned)s.B, segs), dim3(kThreads), 0, st, s, stat, race, (int)segs, n, next);
+    hipLaunchKernelGGL(sd_draw_kernel<T>, dim3((unsigned)s.B, (unsigned)((s.V + kRace - 1) / kRace)), dim3(kThreads), 0, st, s, stat, race, (int)segs, n, next);
 }
 
 }  // namespace
