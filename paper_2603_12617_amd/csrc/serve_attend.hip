@@ -13,13 +13,17 @@
 // 8 (r >> 2) + 4 h + (r & 3) of 32, and since a sum over keys may take them in any order, the V operand is read in
 // that order.  Weights are not moved between lanes or through LDS.
 //
-// Keys and values go from the pages to LDS without passing registers (global_load_lds), one tile ahead of the products,
+// Keys and values go from the pages to LDS without passing registers (global_load_lds), one tile or two ahead of the products,
 // their 16-byte pieces permuted within a row (at the source, LDS order being fixed) so that the reads above find different banks.
 //
 // Two shapes of a workgroup:
-//   kRows wavefronts of 32 rows each over the same tile of 64 keys (prompts' chunks: bound by the matrix units), or
-//   one tile of 32 rows, and kKeys wavefronts with keys of their own that never wait for each other until they are joined in LDS at
-//   the end (decoding: bound by the cache's way from HBM; a wavefront has 16 KB of D = 128 on the way at any time).
+//   four wavefronts of 32 rows each that load and use the same tiles of 64 keys, one tile ahead (LDS: 64 KB at D = 128, two workgroups to a compute unit;
+//   wavefronts without a row only load).  Prompts' chunks, bound by the matrix units: 4 x 2048 tokens of 32 heads over 8192 keys of 8, D = 128: 945 us,
+//   1.0 PFLOP/s of the 1.16 that a large matrix product reaches; the softmax's vector instructions beside the products keep these from
+//   more.  And decoding with keys split to fill the chip, bound by the cache's way from HBM: 2 x 5 tokens over 100000 keys, D = 128, 151 us, 5.4 TB/s
+//   of the 6.1 that a pure read reaches.
+//   one tile of 32 rows, and two wavefronts with 32 keys of their own, two tiles ahead each, that never wait for each other until they are joined in LDS at the
+//   end: decoding of whole requests, of which the long ones end alone on their compute units (64 x 5 tokens over 200 to 4096 keys, 115 us, 5.1 TB/s).
 // Where tiles are few, the range of keys is split over workgroups, and a second kernel joins their parts.
 #include "../../include/specdec.h"
 
@@ -226,13 +230,13 @@ __device__ __forceinline__ float total(float v)
     return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
 }
 
-// A request's tiles of 32 rows, and the steps of keys that they see
+// A request's tiles of rows, and the steps of keys that they see
 struct Work { int tiles, first, steps; };
-__device__ __forceinline__ Work work_of(const Attend &p, int b, int keys)
+__device__ __forceinline__ Work work_of(const Attend &p, int b, int rows, int keys)
 {
     const Rows r = rows_of(p.a, b);
     Work w;
-    w.tiles = (r.m * p.G + 31) / 32;
+    w.tiles = (int)((unsigned)(r.m * p.G) + rows - 1) / rows;
     w.first = see_from(p.a, r, 0) / keys;
     w.steps = r.m ? max((see_to(r, r.m - 1) + keys - 1) / keys - w.first, 0) : 0;
     return w;
@@ -241,7 +245,7 @@ __device__ __forceinline__ Work work_of(const Attend &p, int b, int keys)
 // Workgroups of a key head: every tile of a request, times the parts of at most `per` steps that its keys are split into.  Workgroup x
 // works part `split` of tile `tile` of request b; its parts of a tile are `tiles` places apart.
 struct Unit { int b, tile, split, tiles, splits, per, place; Work w; };
-__device__ __forceinline__ bool unit_of(const Attend &p, int x, int keys, int lane, Unit &u)
+__device__ __forceinline__ bool unit_of(const Attend &p, int x, int rows, int keys, int lane, Unit &u)
 {
     const int B = (int)p.a.B;
     // A lane holds a request, or of more than 64 the sums over a 64th of them
@@ -251,7 +255,7 @@ __device__ __forceinline__ bool unit_of(const Attend &p, int x, int keys, int la
     float all = 0.f;                                         // steps of all workgroups (tiles' parts), for means
     for (int e = 0; e < chunk; ++e)
         if (b0 + e < B) {
-            w = work_of(p, b0 + e, keys);
+            w = work_of(p, b0 + e, rows, keys);
             tiles += w.tiles;
             all += (float)w.tiles * (float)w.steps;
             if (w.tiles) longest = max(longest, w.steps);
@@ -309,7 +313,7 @@ __device__ __forceinline__ bool unit_of(const Attend &p, int x, int keys, int la
         u.place = x;
         int count = 0;
         for (int e = 0; e < chunk; ++e)
-            if (b0 + e < B) { const Work v = work_of(p, b0 + e, keys); count += v.tiles * splits_of(v); }
+            if (b0 + e < B) { const Work v = work_of(p, b0 + e, rows, keys); count += v.tiles * splits_of(v); }
         if (total(count) > p.units) {
             per = longest;
             count = tiles;
@@ -320,7 +324,7 @@ __device__ __forceinline__ bool unit_of(const Attend &p, int x, int keys, int la
         int at = __builtin_ctzll(past);
         x -= __builtin_amdgcn_readlane(sum, at) - __builtin_amdgcn_readlane(count, at);
         const int first = at * chunk;                        // (chunk <= 64: its requests one by one)
-        w = lane < chunk && first + lane < B ? work_of(p, first + lane, keys) : Work{0, 0, 0};
+        w = lane < chunk && first + lane < B ? work_of(p, first + lane, rows, keys) : Work{0, 0, 0};
         count = w.tiles * splits_of(w);
         sum = scan(count);
         past = __ballot(sum > x);
@@ -350,7 +354,7 @@ template <int DK> struct Shape {
     static __device__ __forceinline__ int v_at(int row, int c) { return kPieces >= 16 ? c ^ (4 * (row & 3)) : c ^ (4 * ((row >> 1) & 1)); }
 };
 
-template <typename T, int DK, bool kFull, int kRows, int kKeys, int KT>
+template <typename T, int DK, bool kFull, int kRows, int kKeys, int KT, bool kUnits>
 __global__ void __launch_bounds__(64 * kRows * kKeys, DK > 192 || (kRows == 1 && DK > 128) ? 1 : 2) sd_attend_kernel(const Attend p)
 {
     static_assert(kRows == 1 || kKeys == 1, "wavefronts differ in rows or in keys");
@@ -368,19 +372,18 @@ __global__ void __launch_bounds__(64 * kRows * kKeys, DK > 192 || (kRows == 1 &&
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = kRows > 1 ? wave : 0, wk = kRows > 1 ? 0 : wave;
     const int half = lane >> 5, col = lane & 31;
-    // The chip deals workgroups to its eight dies in turn.  Chunks, grouped: an eighth of the key heads, neighbours, to each die, whose cache then holds their
-    // keys for all tiles of a request, and the lines of memory that neighbouring heads share; where the heads are no multiple of eight, the borders move
-    // from tile to tile.  Otherwise in turn.  Decoding, where keys are read once: the heads of a range of keys one after the other on one die, so
-    // that the pieces of a token's row are fetched at about the same time.
+    // The chip deals workgroups to its eight dies in turn, and so go the heads of a tile, but where neighbouring heads share lines of memory or a
+    // request's tiles its keys (plan_of).  Chunks, grouped: an eighth of the key heads, neighbours, to each die; where the heads are no multiple of
+    // eight, the borders move from tile to tile.  Decoding, grouped: all heads of a range of keys one after the other on one die.
     const unsigned heads = (unsigned)a.cache.heads, die = blockIdx.x % 8, turn = blockIdx.x / 8;
     unsigned item;
     int kh;
-    if (kOwn) {
-        item = turn / heads * 8 + die;
-        kh = turn % heads;
-    } else if (!p.grouped) {
+    if (!p.grouped) {
         item = blockIdx.x / heads;
         kh = blockIdx.x % heads;
+    } else if (kUnits) {
+        item = turn / heads * 8 + die;
+        kh = turn % heads;
     } else {
         const unsigned each = (heads + 7) / 8, shift = 7 - (item = turn / each) % 8;     // (head h is on die (8 h + 7 - shift) / heads)
         kh = (die * heads + shift) / 8 + turn % each;
@@ -390,9 +393,9 @@ __global__ void __launch_bounds__(64 * kRows * kKeys, DK > 192 || (kRows == 1 &&
 
     int b, row0, t0, t1, parts, part_row = 0, part_step = 0, split;      // tiles of keys t0, t0 + kKeys, .. < t1; where the parts of row 0 lie, by rows
     Rows rq;
-    if (kOwn) {
+    if (kUnits) {
         Unit u;
-        if ((int)item >= p.units || !unit_of(p, item, KT * kKeys, lane, u)) return;
+        if ((int)item >= p.units || !unit_of(p, item, kBM, KT * kKeys, lane, u)) return;
         b = u.b;
         rq = rows_of(a, b);
         row0 = kBM * u.tile;
@@ -412,8 +415,8 @@ __global__ void __launch_bounds__(64 * kRows * kKeys, DK > 192 || (kRows == 1 &&
         t0 = t1 = parts = 0;
     }
     const int rows = rq.m * G, tok0 = row0 / G, tok1 = (min(row0 + kBM, rows) - 1) / G;
-    const Span sp = span_of(a, rq, tok0, tok1, KT * kKeys, kOwn ? 1 : p.splits, p.min_steps);
-    if (kOwn) {                                              // (a request's tiles see a little less than all of its keys)
+    const Span sp = span_of(a, rq, tok0, tok1, KT * kKeys, kUnits ? 1 : p.splits, p.min_steps);
+    if (kUnits) {                                              // (a request's tiles see a little less than all of its keys)
         t0 = max(t0, sp.first) * kKeys + wk;
         t1 = min(t1, sp.first + sp.count) * kKeys;
     } else {
@@ -640,7 +643,7 @@ __global__ void __launch_bounds__(64 * kRows * kKeys, DK > 192 || (kRows == 1 &&
 
     const bool whole = parts <= 1;
     const int64_t orow = (int64_t)(rq.first + tok) * a.Hq + head;
-    const int64_t first_part = kOwn ? part_row + col : orow, part_stride = kOwn ? part_step : a.tokens * a.Hq, prow = first_part + split * part_stride;
+    const int64_t first_part = kUnits ? part_row + wm * 32 + col : orow, part_stride = kUnits ? part_step : a.tokens * a.Hq, prow = first_part + split * part_stride;
     if (kKeys > 1) {
         // join the wavefronts: maximum, sum and values of each to LDS, then a share of D to each
         constexpr int kP = DK + 4;                           // floats of a row
@@ -805,20 +808,30 @@ int check(const sd_attention &a)
 }
 
 // ---- which kernel, and how many workgroups: by the shapes alone ----
-struct Plan { int dk, rows, tiles, splits, min_steps, units, once, pairs; bool level, join, grouped; };
+struct Plan { int dk, rows, tiles, splits, min_steps, units, once, pairs; bool many, level, join, grouped; };
 Plan plan_of(const sd_attention &a)
 {
     Plan p;
     const int64_t heads = a.cache.heads, G = a.Hq / heads, D = a.cache.D, rows = a.tokens * G;
+    // heads are padded to the next of these (8 x 512 tokens over 2048 keys: D = 80 in 96 119 us, in 128 134; 144 in 192 200, in 256 374)
     p.dk = D <= 64 ? 64 : D <= 96 ? 96 : D <= 128 ? 128 : D <= 192 ? 192 : 256;
-    // From one and a half tiles of 32 rows a request on, four wavefronts of rows share the keys; below, wavefronts take keys of their own.
-    const bool many = rows > 48 * a.B;
-    p.rows = many ? 128 : 32;
-    const int64_t step = many ? (p.dk <= 128 ? 64 : 32) : (p.dk <= 128 ? 2 : 1) * 32;   // keys
-    const int64_t there = (rows / p.rows > a.B ? rows / p.rows : a.B) * heads;          // workgroups, nothing split
+    // Chunks: more than 32 rows a request and key head (in the mean), so that its keys would be read more than once by tiles of 32, and are shared
+    // by 128 (64 requests of 40 rows over 2000 keys, D = 128: 99 us, in tiles of 32 162; of 32 rows 98 and 106; 8 of 36 over 8000: 53 and 89).
+    const bool many = p.many = rows > 32 * a.B;
+    const int64_t there = (rows / 128 > a.B ? rows / 128 : a.B) * heads;          // workgroups, nothing split
+    // Keys are split where the requests' tiles do not fill the chip, which has room for 512 workgroups.  Chunks: below 256 (8192 keys: 1 x 128 tokens
+    // 38 us, unsplit 152; 1 x 512 90 and 153; but 24 chunks of 40 tokens, 20 heads, 480 workgroups: 67 and 50).  Decoding: below 512, though equal lengths lose
+    // by it (32 requests, 8 heads, 2000 keys each: 50 and 43 us; 200 to 4096: 49 and 76; with 5 tokens 66 and 89; 40 of these 94 and 104).
+    // Decoding of whole requests takes wavefronts with keys of their own where the head fills its row in LDS (64 x 5 tokens, D = 128, 200 to
+    // 4096 keys: 115 us, shared tiles 119; 2000 each: 100 and 98); else (2048 each; D = 80, 96, 144, 192) shared tiles: 64, 75, 110, 143 us to 71, 79, 157, 171.
+    const bool fill = there < (many ? 256 : 512), own = !many && !fill && (D == 64 || D == 128);
+    p.rows = own ? 32 : 128;
+    const int64_t step = p.dk != 192 ? 64 : 32;                                         // keys
     int64_t longest = a.width * a.cache.page;
     if (a.window > 0 && a.window + p.rows / G + 1 < longest) longest = a.window + p.rows / G + 1;
-    p.min_steps = there >= 256 ? 16 : there >= 64 ? 4 : 2;
+    // Short parts where workgroups are few and wait for nothing but their own keys (1 request, 1500 keys, parts of 64, 128, 256, 1024 keys at least: 11.4, 12.3,
+    // 14.3, 26 us); where there are more, the room for workgroups ends the splitting first.
+    p.min_steps = there >= 64 ? 4 : 1;
     const int64_t most = (longest + p.min_steps * step - 1) / (p.min_steps * step);     // parts of the longest context
     p.tiles = (int)(rows / p.rows + a.B);
     p.splits = 1;
@@ -826,7 +839,7 @@ Plan plan_of(const sd_attention &a)
     p.level = p.grouped = false;
     if (many) {
         // a compute unit has room for two workgroups: where they do not fill the chip once, the keys are split
-        int64_t splits = there < 256 ? (512 + there - 1) / there : 1;
+        int64_t splits = fill ? (512 + there - 1) / there : 1;
         splits = splits > most ? most : splits;
         p.splits = (int)(splits > 256 ? 256 : splits < 1 ? 1 : splits);
         p.join = p.splits > 1;
@@ -836,29 +849,34 @@ Plan plan_of(const sd_attention &a)
         p.grouped = heads > 8 && (heads % 8 == 0 || (D % 64 != 0 && a.cache.k_head_stride < a.cache.k_tok_stride));
         return p;
     }
-    // Decoding: where the requests alone do not fill the chip, parts of one length, as many as find room at once.  Contexts far beyond the mean are split in
-    // any case, if the tables are wide enough for such that a workgroup would be long at it (8192 keys of D = 128 take about 170 us).
-    const int64_t once = (512 + heads - 1) / heads < (int64_t)p.tiles * most ? (512 + heads - 1) / heads : (int64_t)p.tiles * most;
-    p.once = there < 512 && most > 1 ? (int)once : 0;
+    // Decoding: parts of one length, as many as find room at once (1024 of them: 2 x 5 tokens over 100000 keys 160 us instead of 151); a context of 512 keys is as
+    // fast whole as split and joined (300 keys: 10.0 and 12.6 us, 400 12.1 and 11.5, 1500 29 and 11.4).  Contexts far beyond the mean are split in
+    // any case, if the tables are wide enough for such that a workgroup would be long at it: 8192 keys of D = 128 take about 170 us, and joining
+    // costs 8 (64 x 5 tokens over 2000 keys 106 and 114 us; 63 requests of 500 keys and one of 60000: 96 us, 1120 unsplit).
+    const int64_t room1 = (512 + heads - 1) / heads, once = room1 < (int64_t)p.tiles * most ? room1 : (int64_t)p.tiles * most;
+    p.once = fill && longest > 512 ? (int)once : 0;
+    // (heads whose pieces share lines of 128 bytes on one die: 64 x 5 tokens over 2048 keys, D = 80 and 96: 64 and 75 us, in turn 81 and 83; D = 128 and 192 103
+    // and 147, in turn 99 and 144)
+    p.grouped = D % 64 != 0 && a.cache.k_head_stride < a.cache.k_tok_stride;
     p.level = longest * D > 8192 * 128;
     const int64_t room = p.tiles + (a.B / 2 > 8 ? a.B / 2 : 8), units = p.level && room > p.once ? room : p.once > p.tiles ? p.once : p.tiles;
-    if (units * heads * 32 > 0x7fffffff) { p.once = 0; p.level = false; }            // (rows of parts are numbered in 32 bits)
+    if (units * heads * p.rows > 0x7fffffff) { p.once = 0; p.level = false; }            // (rows of parts are numbered in 32 bits)
     p.units = p.once || p.level ? (int)units : p.tiles;
-    // A compute unit gets the i-th and the i + 256-th workgroup: a long request next to a short one (64 x 5 tokens over 200 - 4096 keys: 122 us; as they
+    // A compute unit gets the i-th and the i + 256-th workgroup: a long request next to a short one (64 x 5 tokens over 200 to 4096 keys: 122 us; as they
     // come 135, longest first 136).
     p.pairs = there >= 256 ? (int)((256 + heads - 1) / heads) : 0;
     p.join = p.once || p.level;
     return p;
 }
-int64_t part_rows(const sd_attention &a, const Plan &p) { return p.rows == 128 ? (int64_t)p.splits * a.tokens * a.Hq : (int64_t)p.units * a.cache.heads * 32; }
+int64_t part_rows(const sd_attention &a, const Plan &p) { return p.many ? (int64_t)p.splits * a.tokens * a.Hq : (int64_t)p.units * a.cache.heads * p.rows; }
 // parts, (maximum, sum) of each, and where a row's parts are
 size_t part_bytes(const sd_attention &a, const Plan &p) { return p.join ? (size_t)part_rows(a, p) * (a.cache.D + 2) * 4 + (size_t)a.tokens * a.Hq * sizeof(int4) : 0; }
 
-template <typename T, int DK, bool kFull, int kRows, int kKeys, int KT> void launch_shape(const Attend &p, dim3 grid, hipStream_t st)
+template <typename T, int DK, bool kFull, int kRows, int kKeys, int KT, bool kUnits> void launch_shape(const Attend &p, dim3 grid, hipStream_t st)
 {
     constexpr int tiles = kKeys * 4 * KT * Shape<DK>::kPitch, bytes = tiles + (kRows == 1 ? 4 * kIds * kKeys : 0);
     static_assert(kKeys == 1 || kKeys * (64 + 32 * (DK + 4)) * 4 <= tiles, "the join has room");
-    const auto kernel = sd_attend_kernel<T, DK, kFull, kRows, kKeys, KT>;
+    const auto kernel = sd_attend_kernel<T, DK, kFull, kRows, kKeys, KT, kUnits>;
     static const hipError_t once = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
     (void)once;
     hipLaunchKernelGGL(kernel, grid, dim3(64 * kRows * kKeys), bytes, st, p);
@@ -866,12 +884,16 @@ template <typename T, int DK, bool kFull, int kRows, int kKeys, int KT> void lau
 template <typename T, int DK, bool kFull> void launch(const Attend &p, const Plan &plan, hipStream_t st)
 {
     const int64_t heads = p.a.cache.heads, items = (int64_t)plan.tiles * plan.splits;
-    const dim3 grid((unsigned)(plan.rows == 32 ? ((int64_t)plan.units + 7) / 8 * 8 * heads : plan.grouped ? items * ((heads + 7) / 8 * 8) : items * heads));
-    constexpr int kKeys = DK <= 128 ? 2 : 1, KT = DK <= 128 ? 64 : 32;
-    if (plan.rows == 128) launch_shape<T, DK, kFull, 4, 1, KT>(p, grid, st);
-    else launch_shape<T, DK, kFull, 1, kKeys, 32>(p, grid, st);
+    const dim3 grid((unsigned)(!plan.many ? ((int64_t)plan.units + 7) / 8 * 8 * heads : plan.grouped ? items * ((heads + 7) / 8 * 8) : items * heads));
+    // (shared tiles of 64 and 32 keys, 8 x 512 tokens over 2048 keys, D = 64: 88 and 98 us, 128: 140 and 150, 192, where 64 leave no room for a second workgroup: 236 and
+    // 213, 256, where 32 do not either, the accumulators being so many: 306 and 370)
+    constexpr int KT = DK != 192 ? 64 : 32;
+    if (plan.many) launch_shape<T, DK, kFull, 4, 1, KT, false>(p, grid, st);
+    else if (plan.rows == 128) launch_shape<T, DK, kFull, 4, 1, KT, true>(p, grid, st);
+    else if constexpr (kFull && DK <= 128) launch_shape<T, DK, kFull, 1, 2, 32, true>(p, grid, st);
     if (plan.join) {
         const int64_t rows = p.a.tokens * p.a.Hq;
+        // (few rows are as long as one's chain of parts: 1 token over 8000 keys 16.8 us by workgroups, 23.5 by wavefronts; 2560 rows over 2000 keys 38 and 35)
         if (rows <= 1024) hipLaunchKernelGGL((sd_join_kernel<T, 256>), dim3((unsigned)rows), dim3(256), 0, st, p);
         else hipLaunchKernelGGL((sd_join_kernel<T, 64>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, p);
     }
