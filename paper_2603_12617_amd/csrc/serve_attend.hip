@@ -139,39 +139,6 @@ __device__ __forceinline__ Rows rows_of(const sd_attention &a, int b)
     r.count = r.m;
     return r;
 }
-// Tile x of all requests' tiles of rows: its request, and which of that request's it is; false past the last.  By the
-// lanes of a wavefront: sums over a 64th of the requests each, then over those one by one.  Exact, so that the workgroups without a tile are the
-// last ones: workgroups go to the parts of a die in turn, and were every other one without work, half of the chip would be.
-struct Tile { int b, at; };
-__device__ __forceinline__ bool tile_of(const sd_attention &a, int G, int tile, int x, int lane, Tile &out)
-{
-    const int B = (int)a.B;
-    auto tiles = [&](int b) { return (int)(((unsigned)(rows_of(a, b).m * G) + tile - 1) / (unsigned)tile); };
-    int lo = 0, n = B;
-    for (;;) {
-        const int chunk = (n + 63) / 64;
-        int count = 0;
-        for (int e = 0; e < chunk; ++e)
-            if (lane * chunk + e < n) count += tiles(lo + lane * chunk + e);
-        int sum = count;
-#pragma unroll
-        for (int sh = 1; sh < 64; sh <<= 1) {
-            const int other = __shfl_up(sum, sh);
-            if (lane >= sh) sum += other;
-        }
-        const unsigned long long past = __ballot(sum > x);
-        if (past == 0) return false;
-        const int at = __builtin_ctzll(past);
-        x -= __builtin_amdgcn_readlane(sum, at) - __builtin_amdgcn_readlane(count, at);
-        lo += at * chunk;
-        if (chunk == 1) break;
-        n = min(chunk, n - at * chunk);
-    }
-    out.b = lo;
-    out.at = x;
-    return true;
-}
-
 // the keys that a token of a request sees
 __device__ __forceinline__ int see_to(const Rows &r, int tok) { return min(max(r.before + tok + 1, 0), r.kv); }
 __device__ __forceinline__ int see_from(const sd_attention &a, const Rows &r, int tok)
@@ -179,22 +146,6 @@ __device__ __forceinline__ int see_from(const sd_attention &a, const Rows &r, in
     return a.window > 0 ? (int)min((int64_t)r.kv, max((int64_t)0, (int64_t)r.before + tok + 1 - a.window)) : 0;
 }
 
-// The steps (of `keys` keys) of a tile of rows, and those of one of its splits.
-struct Span { int first, count, per, used; };
-__device__ __forceinline__ Span span_of(const sd_attention &a, const Rows &r, int tok0, int tok1, int keys, int splits, int min_steps)
-{
-    Span s;
-    const int lo = see_from(a, r, tok0), hi = see_to(r, tok1);
-    s.first = lo / keys;
-    s.count = hi > lo ? (hi + keys - 1) / keys - s.first : 0;
-    s.per = max((s.count + splits - 1) / splits, min_steps);
-    s.used = (s.count + s.per - 1) / s.per;
-    return s;
-}
-
-constexpr int kMaxParts = 256;     // of a row
-
-// ---- decoding: what a workgroup does ----
 // sums over the lanes up to this one, as lane moves within the wavefront's registers
 template <int CTRL, int ROWS> __device__ __forceinline__ int moved(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xF, false); }
 __device__ __forceinline__ int scan(int v)
@@ -230,6 +181,76 @@ __device__ __forceinline__ float total(float v)
     return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
 }
 
+// Up to 64 requests, one to a lane, each with `count` workgroups of `length`: the counts of those with any, the longest first, and which request each is.
+// (A request without workgroups may stand anywhere: the others close up before it.)
+struct Order { int count, who; };
+__device__ __forceinline__ Order longest_first(int B, int length, int count, int lane)
+{
+    const int key = count ? min(length, 1 << 24) * 64 + 63 - lane : 0;
+    int rank = 0;
+    for (int j = 0; j < B; ++j) rank += __builtin_amdgcn_readlane(key, j) > key;
+    const unsigned long long there = __ballot(count > 0);
+    if (!count) rank = __builtin_popcountll(there) + __builtin_popcountll(~there & ((1ull << lane) - 1));
+    return Order{__builtin_amdgcn_ds_permute(4 * rank, count), __builtin_amdgcn_ds_permute(4 * rank, lane)};
+}
+
+// Tile x of all requests' tiles of rows: its request, and which of that request's it is; false past the last.  By the
+// lanes of a wavefront: sums over a 64th of the requests each, then over those one by one.  Exact, so that the workgroups without a tile are the
+// last ones: workgroups go to the parts of a die in turn, and were every other one without work, half of the chip would be.
+struct Tile { int b, at; };
+__device__ __forceinline__ bool tile_of(const sd_attention &a, int G, int tile, int x, int lane, Tile &out)
+{
+    const int B = (int)a.B;
+    auto tiles = [&](int b) { return (int)(((unsigned)(rows_of(a, b).m * G) + tile - 1) / (unsigned)tile); };
+    if (B <= 64) {
+        // longest requests first, so that the last workgroups to start are short ones (24 x 1 to 301 tokens behind 0 to 3000, 20 heads of 80: 97 us, in order 125)
+        const Rows r = lane < B ? rows_of(a, lane) : Rows{0, 0, 0, 0, 0};
+        const int m = r.m, keys = m ? see_to(r, m - 1) - see_from(a, r, max(m - tile / G, 0)) : 0;
+        const Order o = longest_first(B, max(keys, 0) >> 6, lane < B ? tiles(lane) : 0, lane);
+        const int sum = scan(o.count);
+        const unsigned long long past = __ballot(sum > x);
+        if (past == 0) return false;
+        const int at = __builtin_ctzll(past);
+        out.b = __builtin_amdgcn_readlane(o.who, at);
+        out.at = x - (__builtin_amdgcn_readlane(sum, at) - __builtin_amdgcn_readlane(o.count, at));
+        return true;
+    }
+    int lo = 0, n = B;
+    for (;;) {
+        const int chunk = (n + 63) / 64;
+        int count = 0;
+        for (int e = 0; e < chunk; ++e)
+            if (lane * chunk + e < n) count += tiles(lo + lane * chunk + e);
+        const int sum = scan(count);
+        const unsigned long long past = __ballot(sum > x);
+        if (past == 0) return false;
+        const int at = __builtin_ctzll(past);
+        x -= __builtin_amdgcn_readlane(sum, at) - __builtin_amdgcn_readlane(count, at);
+        lo += at * chunk;
+        if (chunk == 1) break;
+        n = min(chunk, n - at * chunk);
+    }
+    out.b = lo;
+    out.at = x;
+    return true;
+}
+
+// The steps (of `keys` keys) of a tile of rows, and those of one of its splits.
+struct Span { int first, count, per, used; };
+__device__ __forceinline__ Span span_of(const sd_attention &a, const Rows &r, int tok0, int tok1, int keys, int splits, int min_steps)
+{
+    Span s;
+    const int lo = see_from(a, r, tok0), hi = see_to(r, tok1);
+    s.first = lo / keys;
+    s.count = hi > lo ? (hi + keys - 1) / keys - s.first : 0;
+    s.per = max((s.count + splits - 1) / splits, min_steps);
+    s.used = (s.count + s.per - 1) / s.per;
+    return s;
+}
+
+constexpr int kMaxParts = 256;     // of a row
+
+// ---- decoding: what a workgroup does ----
 // A request's tiles of rows, and the steps of keys that they see
 struct Work { int tiles, first, steps; };
 __device__ __forceinline__ Work work_of(const Attend &p, int b, int rows, int keys)
@@ -292,14 +313,9 @@ __device__ __forceinline__ bool unit_of(const Attend &p, int x, int rows, int ke
         }
         int count = mine, who = lane;
         if (p.pairs && B > 1) {                              // in the order of their lengths, longest first
-            const int key = w.tiles ? min(w.steps, 1 << 24) * 64 + 63 - lane : 0;
-            int rank = 0;
-            for (int j = 0; j < B; ++j) rank += __builtin_amdgcn_readlane(key, j) > key;
-            // (a request without rows may stand anywhere: the others close up before it)
-            const unsigned long long there = __ballot(w.tiles > 0);
-            if (!w.tiles) rank = __builtin_popcountll(there) + __builtin_popcountll(~there & ((1ull << lane) - 1));
-            count = __builtin_amdgcn_ds_permute(4 * rank, mine);
-            who = __builtin_amdgcn_ds_permute(4 * rank, lane);
+            const Order o = longest_first(B, w.steps, mine, lane);
+            count = o.count;
+            who = o.who;
         }
         const int sum = scan(count), n = __builtin_amdgcn_readlane(sum, 63);
         if (x >= n) return false;
