@@ -1,7 +1,7 @@
 // Verification of drafted tokens from logits (sd_verify_logits): two launches.
 //
 //   stats   every row of V logits in segments of kSeg, a workgroup each: the largest logit and, of the rows of requests with a
-//           temperature, sum 2^(l c - top c), c = log2(e) / tau, of greedy ones the largest's first place.  All segments are independent,
+//           temperature, sum 2^((l - top) c), c = log2(e) / tau, of greedy ones the largest's first place.  All segments are independent,
 //           so a batch of one request fills V / kSeg workgroups a row and a large one the chip; each logit is read once.
 //   draw    per request and kRace places: the rows' partial sums are joined (again by every workgroup of the request: a few
 //           hundred numbers from L2, in a fixed order, half a wavefront to a row), the drafts tested, and these places of row n
@@ -13,9 +13,11 @@
 // 700 MB, 5.5 TB/s of the 6.1 that a pure read reaches, and 61 us for the draw's 289 MB, 4.7 TB/s behind a chain of dependent reads.  8 of 4,
 // V = 32000, float: 4.8 and 7.8 us, the launch and such chains.
 //
-// c is kept as a sum of two floats: its own rounding would move all weights of a row together, by |l - top| c 6e-8.  The low part is
-// positive, so that l = -inf gives a weight of 0 without a test.  What these few instructions cannot do (NaN, +inf, products beyond
-// the float range) shows in a workgroup's maximum and sum, and is done again one by one.
+// The difference is taken before it is multiplied: of l c - top c each part would be rounded in units of its own size, which for masks of -1e10
+// or temperatures of 1e-8 are powers of two of 1 and more.  So the largest logit's weight is 1 whatever its size, no sum is more than its
+// number of places, and weights of all segments are relative to the same exact number.  c is kept as a sum of two floats: its own rounding would move
+// all weights of a row together, by |l - top| c 6e-8.  The low part is positive, so that l = -inf gives a weight of 0 without a test.  What these few
+// instructions cannot do (NaN, +inf, rows of -inf) shows in a workgroup's maximum and sum, and is done again one by one.
 #include "../../include/specdec.h"
 
 #include <hip/hip_runtime.h>
@@ -33,7 +35,7 @@ constexpr int kSeg = kThreads * kPer;          // of a workgroup
 constexpr int kRacePer = 16;
 constexpr int kRace = kThreads * kRacePer;
 constexpr int kMaxSegs = (SD_MAX_V + kSeg - 1) / kSeg;
-constexpr float kNone = -__builtin_inff();
+constexpr float kNone = -__builtin_inff(), kLargest = 3.4028234663852886e38f;
 static_assert(kMaxSegs <= 32, "half a wavefront joins a row");
 
 struct Stat { float top, sum; int at; };       // of a row's segment
@@ -90,28 +92,27 @@ template <typename T> __device__ __forceinline__ typename Vec<T>::Raw load(const
 template <typename T, int size> __device__ __forceinline__ int place(int seg, int c) { return seg * size + (c * kThreads + (int)threadIdx.x) * Vec<T>::kVec; }
 
 // NaN counts as -inf, +inf as the largest float
-__device__ __forceinline__ float clean(float l) { return l == l ? fminf(l, 3.4028234663852886e38f) : kNone; }
+__device__ __forceinline__ float clean(float l) { return l == l ? fminf(l, kLargest) : kNone; }
 
 // ---- temperature ----
 struct Heat { float hi, lo; };                 // log2(e) / tau as a sum, lo > 0
 __device__ __forceinline__ Heat heat(float tau)
 {
-    const double c = fmax(fmin(1.4426950408889634 / (double)tau, 1e30), 1e-30);
+    const double c = fmax(fmin(1.4426950408889634 / (double)tau, 1e38), 1e-30);
     Heat h;
     h.hi = (float)c;
     if ((double)h.hi > c) h.hi = __uint_as_float(__float_as_uint(h.hi) - 1);
     h.lo = fmaxf((float)(c - (double)h.hi), 1e-37f);
     return h;
 }
-// whether l c - top c stays in the float range for every l <= top
-__device__ __forceinline__ bool tame(float top, Heat h) { return fabsf(top * h.hi) < 1e30f; }
-__device__ __forceinline__ float power(float l, float ref, Heat h) { return __builtin_amdgcn_exp2f(__builtin_fmaf(l, h.lo, __builtin_fmaf(l, h.hi, -ref))); }
-// the same of any clean logit (below 2^-125 of the largest: 0)
-__device__ __forceinline__ float power_any(float l, float top, Heat h)
+// the weight of a logit in a row whose largest is `top`, both finite, or l = -inf
+__device__ __forceinline__ float power(float l, float top, Heat h)
 {
     const float d = l - top;
-    return d * h.hi >= -125.f ? __builtin_amdgcn_exp2f(__builtin_fmaf(d, h.lo, d * h.hi)) : 0.f;
+    return __builtin_amdgcn_exp2f(__builtin_fmaf(d, h.lo, d * h.hi));
 }
+// the same of any clean logits
+__device__ __forceinline__ float power_any(float l, float top, Heat h) { return l > kNone ? power(l, top, h) : 0.f; }
 
 // ---- reductions by lane moves within the wavefront's registers (a trip through LDS per step would be the larger part of a small call) ----
 // lanes without a source, and rows outside ROWS, get `none`
@@ -202,24 +203,16 @@ __global__ void __launch_bounds__(kThreads) sd_stats_kernel(const sd_logits s, S
     int at = 0x7fffffff;
     float sum = 0.f;
     if (hot) {
-        const float ref = top * h.hi;
-        bool odd = !tame(top, h);
-        if (!odd) {
 #pragma unroll
-            for (int c = 0; c < kC; ++c)
+        for (int c = 0; c < kC; ++c)
 #pragma unroll
-                for (int e = 0; e < E::kVec; ++e) sum += power(E::get(raw[c], e), ref, h);
-            odd = sum != sum;
-        }
-        if (odd) {
+            for (int e = 0; e < E::kVec; ++e) sum += power(E::get(raw[c], e), top, h);
+        if (sum != sum) {
             sum = 0.f;
 #pragma unroll
             for (int c = 0; c < kC; ++c)
 #pragma unroll
-                for (int e = 0; e < E::kVec; ++e) {
-                    const float v = clean(E::get(raw[c], e));
-                    sum += tame(top, h) ? power(v, ref, h) : power_any(v, clean(top), h);
-                }
+                for (int e = 0; e < E::kVec; ++e) sum += power_any(clean(E::get(raw[c], e)), clean(top), h);
         }
     } else {
 #pragma unroll
@@ -251,12 +244,7 @@ __device__ __forceinline__ Row join(const Stat &r, Heat h, int lane)
 {
     const float top = of_half(over_half(r.top, kNone, kMax), lane);
     const int best = of_half(over_half(r.top == top ? r.at : 0x7fffffff, 0x7fffffff, kMin), lane);
-    // (sums are relative to top c rounded to float where that is tame)
-    double sum = 0.0;
-    if (r.top > kNone) {
-        const float back = tame(top, h) && tame(r.top, h) ? exp2f((float)((double)(r.top * h.hi) - (double)(top * h.hi))) : power_any(r.top, top, h);
-        sum = (double)r.sum * (double)back;
-    }
+    double sum = (double)r.sum * (double)power_any(r.top, top, h);
     sum = of_half(over_half(sum, 0.0, kSum), lane);
     Row w;
     w.top = top;
@@ -266,10 +254,7 @@ __device__ __forceinline__ Row join(const Stat &r, Heat h, int lane)
 }
 
 // a probability
-__device__ __forceinline__ float weight(float l, const Row &r, Heat h)
-{
-    return (tame(r.top, h) && l == l ? power(l, r.top * h.hi, h) : power_any(clean(l), r.top, h)) * r.inv;
-}
+__device__ __forceinline__ float weight(float l, const Row &r, Heat h) { return power_any(clean(l), r.top, h) * r.inv; }
 
 // larger scores win, of equal ones the lowest place
 __device__ __forceinline__ u64 entry(float score, int x) { return ((u64)__float_as_uint(score) << 32) | (0xffffffffu - (unsigned)x); }
@@ -366,15 +351,14 @@ __global__ void __launch_bounds__(kThreads) sd_draw_kernel(const sd_logits s, co
     const int drafted = rejected && !Q ? min(max(s.tok[first + n], 0), V - 1) : -1;
     float won = 0.f;
     int at = 0;
-    if (tame(p.top, h) && tame(q.top, h)) {
-        const float pref = p.top * h.hi, qref = q.top * h.hi;
+    if (fmaxf(p.top, q.top) < kLargest) {
 #pragma unroll
         for (int c = 0; c < kC; ++c)
 #pragma unroll
             for (int i = 0; i < E::kVec; ++i) {
-                float w = power(E::get(f[c], i), pref, h) * p.inv;
+                float w = power(E::get(f[c], i), p.top, h) * p.inv;
                 // (the maximum takes what is no number for 0; q.inv = 0 without a rejected draft's row)
-                if (qrow) w = __builtin_fmaf(fmaxf(power(E::get(g[c], i), qref, h), 0.f), -q.inv, w);
+                if (qrow) w = __builtin_fmaf(fmaxf(power(E::get(g[c], i), q.top, h), 0.f), -q.inv, w);
                 else if (drafted == place<T, kRace>(seg, c) + i) w = 0.f;
                 const float sc = w * __builtin_amdgcn_rcpf(e[(c * E::kVec + i) / 4][i % 4]);
                 if (sc > won) { won = sc; at = c * E::kVec + i; }     // (places ascend within a thread: of equal scores the first stays)

@@ -1,0 +1,66 @@
+"""Operators of a served verification step where they can go wrong: masks and temperatures of verification, requests that a step refuses,
+streams, weights of very different sizes, and a whole step in a graph."""
+import numpy as np
+import pytest
+import test_gpu_serve as G
+
+from oracle import serve_oracle as SO
+from paper_2603_12617_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+
+
+def _torch():
+    import torch
+    return torch
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("mask", [-1e5, -1e9, -1e10, -1e12, -1e15, -1e20, -1e30])
+@pytest.mark.parametrize("tau", [(0.6, 1.2), (0.05, 0.3)])
+@pytest.mark.parametrize("draft", [True, False])
+def test_masks_that_are_finite(dtype, mask, tau, draft):
+    """All places of a row but a few hundred hold a mask: whole segments of nothing else."""
+    rng = np.random.default_rng(int(-np.log10(-mask)) + 40)
+    V = 3 * 8192 + 100
+    d = G._logits(rng, [2] * 40, V, dtype, draft, tau=tau)
+    keep = rng.permutation(4000)[:300]
+    hide = np.ones(V, bool)
+    hide[keep] = False
+    d["p"][:, hide] = mask
+    if draft:
+        d["q"][:, hide] = mask
+    # drafts are drawn from their rows (a token of probability 1e-50 would be 0 in 32 bits, and then nothing is rejected)
+    rows = d["q"] if draft else d["p"][np.setdiff1d(np.arange(120), d["cu"][1:] - 1)]
+    heat = np.repeat(d["tau"], 2)[:, None]
+    d["tok"] = (rows.double().numpy() / heat + rng.gumbel(size=(80, V))).argmax(1).astype(np.int32)
+    print("case", dtype, mask, tau, draft, flush=True)
+    _, nx = G._check_verify(d)
+    assert np.isin(nx, keep).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("V", [3000, 20000])
+@pytest.mark.parametrize("tau", [1e-4, 1e-6, 1e-8, 1e-9, 1e-12, 1e-20, 1e-36])
+def test_small_temperatures(dtype, V, tau):
+    """Temperatures at which a row is as good as greedy, but for logits that are equal."""
+    rng = np.random.default_rng(V)
+    d = G._logits(rng, [3] * 30, V, dtype, tau=(tau, tau))
+    d["p"] += 5.0
+    d["tok"] = d["q"].float().argmax(1).numpy().astype(np.int32)
+    print("case", dtype, V, tau, flush=True)
+    n, _ = G._check_verify(d)
+    assert n.max() > 0
+
+
+@pytest.mark.parametrize("shift", [-1e7, -7.3e5, 7.2e5, 7.3e5, 3e6, 1e7])
+def test_logits_far_from_zero(shift):
+    """A row's probabilities do not depend on a number that is added to all of its logits (these sums are exact)."""
+    rng = np.random.default_rng(3)
+    d = G._logits(rng, [2] * 40, 10000, "f32")
+    d["p"], d["q"] = d["p"].round() + shift, d["q"].round() + shift
+    d["p"][:, 5000:] -= 8.0
+    print("case", shift, flush=True)
+    G._check_verify(d)
