@@ -253,6 +253,14 @@ __device__ __forceinline__ Row join(const Stat &r, Heat h, int lane)
     return w;
 }
 
+// w - v i with the product rounded by itself, as w's was: equal rows leave nothing
+__device__ __forceinline__ float less(float w, float v, float i)
+{
+#pragma clang fp contract(off)
+    const float x = v * i;
+    return w - x;
+}
+
 // a probability
 __device__ __forceinline__ float weight(float l, const Row &r, Heat h) { return power_any(clean(l), r.top, h) * r.inv; }
 
@@ -357,8 +365,8 @@ __global__ void __launch_bounds__(kThreads) sd_draw_kernel(const sd_logits s, co
 #pragma unroll
             for (int i = 0; i < E::kVec; ++i) {
                 float w = power(E::get(f[c], i), p.top, h) * p.inv;
-                // (the maximum takes what is no number for 0; q.inv = 0 without a rejected draft's row)
-                if (qrow) w = __builtin_fmaf(fmaxf(power(E::get(g[c], i), q.top, h), 0.f), -q.inv, w);
+                // (the maximum takes what is no number for 0)
+                if (qrow) w = less(w, fmaxf(power(E::get(g[c], i), q.top, h), 0.f), q.inv);
                 else if (drafted == place<T, kRace>(seg, c) + i) w = 0.f;
                 const float sc = w * __builtin_amdgcn_rcpf(e[(c * E::kVec + i) / 4][i % 4]);
                 if (sc > won) { won = sc; at = c * E::kVec + i; }     // (places ascend within a thread: of equal scores the first stays)
@@ -369,7 +377,7 @@ __global__ void __launch_bounds__(kThreads) sd_draw_kernel(const sd_logits s, co
 #pragma unroll
             for (int i = 0; i < E::kVec; ++i) {
                 float w = weight(E::get(f[c], i), p, h);
-                if (qrow) w -= weight(E::get(g[c], i), q, h);
+                if (qrow) w = less(w, power_any(clean(E::get(g[c], i)), q.top, h), q.inv);
                 else if (drafted == place<T, kRace>(seg, c) + i) w = 0.f;
                 const float sc = w * __builtin_amdgcn_rcpf(e[(c * E::kVec + i) / 4][i % 4]);
                 if (sc > won) { won = sc; at = c * E::kVec + i; }

@@ -64,3 +64,30 @@ def test_logits_far_from_zero(shift):
     d["p"][:, 5000:] -= 8.0
     print("case", shift, flush=True)
     G._check_verify(d)
+
+
+@pytest.mark.parametrize("V", [700, 5000, 20000])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_residual_of_equal_rows_is_nothing(V, dtype):
+    """The draft's row is the target's, and yet its draft is rejected (by a number outside [0, 1)): the draw is from the target's row."""
+    rng = np.random.default_rng(V)
+    d = G._logits(rng, [1] * 25, V, dtype)
+    d["q"] = d["p"][d["cu"][:-1]].clone()
+    d["r"][:] = 3.0
+    n, nx = G._check_verify(d)
+    assert (n == 0).all() and len(set(nx.tolist())) > 5
+
+
+@pytest.mark.parametrize("V", [64, 5000, 20000])
+def test_residual_without_the_only_possible_token(V):
+    """All of a row's mass lies on a draft without a distribution, which is rejected: it is drawn all the same."""
+    rng = np.random.default_rng(V)
+    d = G._logits(rng, [1] * 6, V, "f32", False)
+    for b in range(6):
+        at = int(rng.integers(0, V))
+        row = d["cu"][b]
+        d["p"][row] = -float("inf")
+        d["p"][row, at] = 1.0
+        d["tok"][b], d["r"][b] = at, 1.5
+    n, nx = G._run_verify(d)
+    assert (n == 0).all() and nx.tolist() == d["tok"].tolist()
