@@ -92,6 +92,7 @@ def verify_logits(p, q, tok, r, noise, tau, cu):
         k, first = int(cu[b + 1]) - int(cu[b]) - 1, int(cu[b]) - b
         rows = np.array(p[cu[b]:cu[b + 1]], np.float64)
         rows[np.isnan(rows)] = -np.inf
+        rows = np.minimum(rows, np.finfo(np.float32).max)
         x = np.clip(np.asarray(tok[first:first + k], np.int64), 0, V - 1)
         if not tau[b] > 0:
             best = rows.argmax(axis=1)

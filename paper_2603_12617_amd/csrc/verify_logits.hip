@@ -215,11 +215,12 @@ __global__ void __launch_bounds__(kThreads) sd_stats_kernel(const sd_logits s, S
                 for (int e = 0; e < E::kVec; ++e) sum += power_any(clean(E::get(raw[c], e)), clean(top), h);
         }
     } else {
+        const float most = clean(top);         // (of +inf and the largest float the first one counts)
 #pragma unroll
         for (int c = kC - 1; c >= 0; --c)
 #pragma unroll
             for (int e = E::kVec - 1; e >= 0; --e)
-                if (E::get(raw[c], e) == top) at = place<T, kSeg>(seg, c) + e;
+                if (E::get(raw[c], e) >= most) at = place<T, kSeg>(seg, c) + e;
     }
     if (hot) sum = over_all(sum, 0.f, kSum); else at = over_all(at, 0x7fffffff, kMin);
     if (lane == 0) { at_sh[wave] = at; sum_sh[wave] = sum; }

@@ -91,3 +91,20 @@ def test_residual_without_the_only_possible_token(V):
         d["tok"][b], d["r"][b] = at, 1.5
     n, nx = G._run_verify(d)
     assert (n == 0).all() and nx.tolist() == d["tok"].tolist()
+
+
+@pytest.mark.parametrize("V", [40, 9000])
+def test_infinite_logits_are_the_largest_number(V):
+    """+inf counts as the largest float, so of the two the first place wins a greedy row."""
+    big = np.finfo(np.float32).max
+    p = np.random.default_rng(V).standard_normal((4, V)).astype(np.float32)
+    p[0, [3, 10]] = big, np.inf
+    p[1, [3, 10]] = np.inf, big
+    p[2, [7, V - 1]] = big, np.inf
+    p[3, [V - 2, V - 1]] = np.inf, np.inf
+    none = np.zeros(0, np.int32)
+    d = dict(p=_torch().tensor(p), q=None, tok=none, r=none.astype(np.float32), noise=np.ones((4, V), np.float32), tau=np.zeros(4, np.float32),
+             cu=np.arange(5, dtype=np.int32))
+    for tau in (0.0, 0.7):                                  # (equal noise: the first of equal weights)
+        d["tau"][:] = tau
+        assert G._run_verify(d)[1].tolist() == [3, 3, 7, V - 2], tau
