@@ -91,13 +91,17 @@ int sd_acceptance(const float *p_dev, const float *q_dev, int64_t B, int64_t k, 
 /*
  * Block tables and slot maps of a step.  All integers; the result does not depend on how the work is
  * divided.  With keep_b the valid tokens of request b and want_b the pages that it needs,
- *   keep_b = min(length[b] + (accepted ? accepted[b] + 1 : 0), pages[b] * page),
+ *   keep_b = min(length[b] + (accepted ? max(accepted[b], -1) + 1 : 0), pages[b] * page),
  *   want_b = ceil((keep_b + add[b]) / page):
- * pages of requests with want_b < pages[b] (rejected drafts; finished requests: length = add = 0)
+ * pages of requests with want_b < pages[b] (rejected drafts; finished requests: length = add = 0, accepted = -1 or NULL)
  * are pushed onto the stack of free pages, requests in order, pages in ascending place; then the others
  * take theirs from its top, requests in order.  A request with want_b > width is refused, and so is, from
  * the first one that finds too few pages on, every request that needs more than it holds: it keeps
  * its pages, and its tokens get slot and position -1.
+ *
+ * Of a refused request (kv_out[b] = length_out[b] with add[b] > 0) no new key is in the cache.  What sd_attend and sd_verify_logits
+ * write for its rows then means nothing, and the caller has to give accepted[b] = -1 in the next step, which says that nothing of the last chunk stands,
+ * the token before its drafts no more than they; the request stays where it was and may bring the same tokens again.
  *
  * Reads only table entries below pages[b] and stack entries below *nfree, and writes only others,
  * so a call can be repeated with the same inputs.  No output may be one of the inputs.
@@ -110,7 +114,7 @@ typedef struct {
     int64_t tokens;               /* entries of slot_out and pos_out: the sum of add, or more (the rest gets -1), or fewer (tokens past them are left out) */
     const int32_t *pages;         /* [B] pages held */
     const int32_t *length;        /* [B] tokens that were valid before the last step's chunk */
-    const int32_t *accepted;      /* [B] accepted drafts of the last step; NULL: length is what is valid */
+    const int32_t *accepted;      /* [B] accepted drafts of the last step; -1 (or below), NULL: length is what is valid */
     const int32_t *add;           /* [B] new tokens */
     const int32_t *nfree;         /* [1] free pages */
     int32_t *table;               /* [B][width] in place */

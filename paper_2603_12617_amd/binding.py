@@ -463,7 +463,7 @@ def sd_pages(pages, length, add, table, free, nfree, page, pages_out, length_out
              accepted=None, stream=None) -> None:
     """Block tables and slot maps of a step.  pages, length, add, accepted [B] i32; table [B][width] i32 and free [pool] i32 are
     updated in place; nfree, nfree_out [1]; pages_out, length_out, kv_out [B], cu_out [B+1], slot_out, pos_out [tokens] i32 are
-    written (tokens: the sum of add).  Asynchronous."""
+    written (tokens: the sum of add).  accepted -1: nothing of a request's last chunk stands (it was refused, kv_out = length_out).  Asynchronous."""
     B, width = table.shape
     T, pool, i32 = slot_out.numel(), free.numel(), (_SD_DTYPE or _sd_types())["i32"]
     _want_all(i32, B, "pages length add pages_out length_out kv_out", pages, length, add, pages_out, length_out, kv_out)

@@ -30,10 +30,9 @@ __device__ __forceinline__ Need need_of(const Step &p, int b)
 {
     const sd_page_step &s = p.s;
     Need r;
-    const int pages = s.pages[b], length = s.length[b], accepted = s.accepted ? s.accepted[b] : -1, add = s.add[b];
+    const int pages = s.pages[b], length = s.length[b], accepted = s.accepted ? max(s.accepted[b], -1) : -1, add = s.add[b];
     r.held = min(max(pages, 0), (int)s.width);
-    const unsigned more = s.accepted ? (unsigned)max(accepted, 0) + 1 : 0;
-    r.keep = (int)min((unsigned)max(length, 0) + more, (unsigned)(r.held * (int)s.page));
+    r.keep = (int)min((unsigned)max(length, 0) + (unsigned)accepted + 1u, (unsigned)(r.held * (int)s.page));
     r.add = min(max(add, 0), 0x7fffffff / (int)s.B);
     const int x = (int)min((unsigned)r.keep + (unsigned)r.add, 0x7fffffffu);
     r.want = x ? min(page_of(p, x - 1) + 1, (int)s.width + 1) : 0;

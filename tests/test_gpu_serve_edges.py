@@ -108,3 +108,36 @@ def test_infinite_logits_are_the_largest_number(V):
     for tau in (0.0, 0.7):                                  # (equal noise: the first of equal weights)
         d["tau"][:] = tau
         assert G._run_verify(d)[1].tolist() == [3, 3, 7, V - 2], tau
+
+
+@pytest.mark.parametrize("Bn,page", [(1, 16), (40, 16), (300, 7)])
+def test_steps_of_which_nothing_stands(Bn, page):
+    """accepted = -1: not even the token before the drafts is kept; below that it counts as -1."""
+    rng = np.random.default_rng(Bn + page)
+    st = G._pages_state(rng, Bn, page, 40, 3000, 150, rng.integers(0, 9, Bn), held_extra=2)
+    acc = rng.integers(-1, 4, Bn)
+    acc[0] = -1
+    want = SO.pages(accepted=acc, page=page, **{**st, "nfree": int(st["nfree"][0])})
+    assert want["length"][0] == st["length"][0]
+    G._same_pages(G._run_pages(st, page, acc), want)
+    G._same_pages(G._run_pages(st, page, np.where(acc == -1, -(1 << 31), acc)), want)
+
+
+def test_a_refused_request_goes_on_where_it_stood():
+    """Three requests, one page left for two that need one: the refused one keeps its length, and gets its tokens' slots a step later, once
+    the third has given its page back."""
+    page = 16
+    st = dict(pages=np.array([1, 1, 1]), length=np.array([14, 14, 9]), add=np.array([5, 5, 5]), table=np.array([[4, -1], [2, -1], [1, -1]]),
+              free=np.array([3, -1, -1, -1, -1]), nfree=np.array([1]))
+    one = G._run_pages(st, page)
+    assert one["kv"].tolist() == [19, 14, 14] and (one["slot"][5:10] == -1).all() and (one["slot"][10:] >= 0).all()
+    refused = (one["kv"] == one["length"]) & (st["add"] > 0)
+    assert refused.tolist() == [False, True, False]
+    accepted = np.where(refused, -1, [1, 3, 0])              # (whatever verification says of rows that are not in the cache)
+    add = np.array([0, 5, 0])
+    length = one["length"].copy()
+    length[2], accepted[2] = 0, -1                           # the third request has ended
+    two = G._run_pages(dict(pages=one["pages"], length=length, add=add, table=one["table"], free=one["free"], nfree=one["nfree"]), page, accepted)
+    assert two["length"].tolist() == [16, 14, 0] and two["kv"].tolist() == [16, 19, 0] and two["pages"].tolist() == [1, 2, 0]
+    assert two["pos"].tolist() == [14, 15, 16, 17, 18] and two["slot"][:2].tolist() == [2 * page + 14, 2 * page + 15]
+    assert two["slot"][2] == two["table"][1, 1] * page and (two["slot"] >= 0).all()
