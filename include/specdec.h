@@ -105,7 +105,7 @@ int sd_acceptance(const float *p_dev, const float *q_dev, int64_t B, int64_t k, 
  *
  * Reads only table entries below pages[b] and stack entries below *nfree, and writes only others,
  * so a call can be repeated with the same inputs.  No output may be one of the inputs.
- * B <= SD_MAX_REQUESTS; pool * page, width * page and width * B below 2^31.
+ * B <= SD_MAX_REQUESTS; pool * page, width * page and width * B below 2^31.  Row offsets that would pass 2^31 - 1 end there.
  */
 typedef struct {
     int64_t B, page;              /* requests; tokens of a page */

@@ -33,23 +33,27 @@ __device__ __forceinline__ Need need_of(const Step &p, int b)
     const int pages = s.pages[b], length = s.length[b], accepted = s.accepted ? max(s.accepted[b], -1) : -1, add = s.add[b];
     r.held = min(max(pages, 0), (int)s.width);
     r.keep = (int)min((unsigned)max(length, 0) + (unsigned)accepted + 1u, (unsigned)(r.held * (int)s.page));
-    r.add = min(max(add, 0), 0x7fffffff / (int)s.B);
-    const int x = (int)min((unsigned)r.keep + (unsigned)r.add, 0x7fffffffu);
-    r.want = x ? min(page_of(p, x - 1) + 1, (int)s.width + 1) : 0;
+    r.add = max(add, 0);
+    const unsigned x = (unsigned)r.keep + (unsigned)r.add;
+    r.want = x > (unsigned)(s.width * s.page) ? (int)s.width + 1 : x ? page_of(p, (int)(x - 1)) + 1 : 0;
     r.back = max(r.held - r.want, 0);
     r.need = r.want <= s.width ? max(r.want - r.held, 0) : 0;
     return r;
 }
 
-__device__ __forceinline__ int wave_scan(int v, int lane)
+// sums over the lanes up to this one
+template <typename F> __device__ __forceinline__ int wave_scan(int v, int lane, F f)
 {
 #pragma unroll
     for (int sh = 1; sh < 64; sh <<= 1) {
         const int o = __shfl_up(v, sh);
-        if (lane >= sh) v += o;
+        if (lane >= sh) v = f(v, o);
     }
     return v;
 }
+// of tokens: sums that would pass 31 bits end there (pages are no more than the tables hold)
+constexpr auto kTokens = [](int a, int b) { return (int)min((unsigned)a + (unsigned)b, 0x7fffffffu); };
+constexpr auto kPages = [](int a, int b) { return a + b; };
 
 // the last request whose sum before it is <= x: sums are ascending, sum[0] = 0
 __device__ __forceinline__ int find(const int *sum, int B, int x)
@@ -77,16 +81,18 @@ __global__ void __launch_bounds__(kThreads) sd_pages_kernel(const Step p)
     int a = first_need.add, f = first_need.back, t = first_need.need;
     for (int e = 1; e < per; ++e) {
         const int b = tid * per + e;
-        if (b < B) { const Need r = need_of(p, b); a += r.add; f += r.back; t += r.need; }
+        if (b < B) { const Need r = need_of(p, b); a = kTokens(a, r.add); f += r.back; t += r.need; }
     }
     const int nfree = min(max(s.nfree[0], 0), (int)s.pool);
-    const int ia = wave_scan(a, lane), iff = wave_scan(f, lane), it = wave_scan(t, lane);
+    const int ia = wave_scan(a, lane, kTokens), iff = wave_scan(f, lane, kPages), it = wave_scan(t, lane, kPages);
     if (lane == 63) { part[0][wave] = ia; part[1][wave] = iff; part[2][wave] = it; }
+    int ea = __shfl_up(ia, 1);                               // (a sum that has ended cannot be taken back)
+    if (lane == 0) ea = 0;
     __syncthreads();
-    int ea = ia - a, ef = iff - f, et = it - t, all_add = 0, all_back = 0, all_need = 0;
+    int ef = iff - f, et = it - t, all_add = 0, all_back = 0, all_need = 0;
     for (int w = 0; w < kWaves; ++w) {
-        if (w < wave) { ea += part[0][w]; ef += part[1][w]; et += part[2][w]; }
-        all_add += part[0][w];
+        if (w < wave) { ea = kTokens(ea, part[0][w]); ef += part[1][w]; et += part[2][w]; }
+        all_add = kTokens(all_add, part[0][w]);
         all_back += part[1][w];
         all_need += part[2][w];
     }
@@ -99,12 +105,12 @@ __global__ void __launch_bounds__(kThreads) sd_pages_kernel(const Step p)
         cu[b] = ea; back[b] = ef; taken[b] = et; keep[b] = r.keep; pages[b] = served ? r.held : ~r.held;
         if (blockIdx.x == 0) {
             s.cu_out[b] = ea;
-            if (b == B - 1) s.cu_out[B] = ea + r.add;
+            if (b == B - 1) s.cu_out[B] = kTokens(ea, r.add);
             s.length_out[b] = r.keep;
             s.kv_out[b] = served ? r.keep + r.add : r.keep;
             s.pages_out[b] = served ? r.want : r.held;
         }
-        ea += r.add; ef += r.back; et += r.need;
+        ea = kTokens(ea, r.add); ef += r.back; et += r.need;
     }
     __syncthreads();
 
@@ -143,7 +149,7 @@ __global__ void __launch_bounds__(kThreads) sd_pages_kernel(const Step p)
             const int i = (int)i0 + e, was = b;
             while (b + 1 < B && cu[b + 1] <= i) ++b;
             const int held = pages[b];
-            const int x = keep[b] + (i - cu[b]), at = page_of(p, x);
+            const int x = (int)((unsigned)keep[b] + (unsigned)(i - cu[b])), at = page_of(p, x);
             slot[e] = pos[e] = -1;
             if (held >= 0 && i < all_add && at < s.width) {
                 if (at != place || b != was) {

@@ -141,3 +141,22 @@ def test_a_refused_request_goes_on_where_it_stood():
     assert two["length"].tolist() == [16, 14, 0] and two["kv"].tolist() == [16, 19, 0] and two["pages"].tolist() == [1, 2, 0]
     assert two["pos"].tolist() == [14, 15, 16, 17, 18] and two["slot"][:2].tolist() == [2 * page + 14, 2 * page + 15]
     assert two["slot"][2] == two["table"][1, 1] * page and (two["slot"] >= 0).all()
+
+
+def test_a_long_chunk_among_many_requests():
+    """One request of 4096 brings 600000 tokens: more than 2^31 / 4096, and no more than a step may have."""
+    rng = np.random.default_rng(11)
+    st = G._pages_state(rng, 4096, 16, 9, 9000, 100, rng.integers(0, 3, 4096))
+    st["add"][7] = 600000                                    # (too long for its table: refused, and still its tokens have their places)
+    want = SO.pages(page=16, **{**st, "nfree": 9000})
+    assert want["cu"][8] - want["cu"][7] == 600000
+    G._same_pages(G._run_pages(st, 16), want)
+
+
+def test_new_tokens_beyond_32_bits_stay_in_the_arrays():
+    """Sums of new tokens past 2^31 - 1 end there."""
+    st = dict(pages=np.array([1, 1, 1, 0]), length=np.array([3, 3, 3, 0]), add=np.array([5, 0x7fffffff, 0x7ffffff0, 9]), table=np.array([[4, -1], [2, -1], [1, -1], [-1, -1]]),
+              free=np.array([3, 0, -1, -1, -1]), nfree=np.array([2]))
+    got = G._run_pages(st, 16, tokens=20)
+    assert got["cu"].tolist() == [0, 5, 0x7fffffff, 0x7fffffff, 0x7fffffff] and got["kv"].tolist() == [8, 3, 3, 9] and got["nfree"].tolist() == [1]
+    assert got["pos"].tolist() == [3, 4, 5, 6, 7] + [-1] * 15 and got["slot"][:5].tolist() == [67, 68, 69, 70, 71] and (got["slot"][5:] == -1).all()
