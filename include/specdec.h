@@ -158,7 +158,8 @@ int sd_cache_store(const sd_cache *cache, const void *k, int64_t k_tok_stride, i
  * token of the chunk, the edge of the window) those others see nothing if its value is finite; one that is not may turn their results
  * into NaN too, since a weight of 0 multiplies it.
  * SD_BF16 and SD_F16; scores, softmax and sums are float32, the weights are rounded to the cache's type
- * before they multiply the values.  D a multiple of 8, at most SD_MAX_HEAD_DIM; rows of D elements and all
+ * before they multiply the values (in float16 those below 2^-21 of a row's largest lose bits, and below 2^-32 they vanish there, though not
+ * from the sum that divides).  D a multiple of 8, at most SD_MAX_HEAD_DIM; rows of D elements and all
  * strides 16-byte aligned.
  * `ws` (16-byte aligned) needs sd_attend_workspace_bytes.  It holds parts of rows whose keys are split over workgroups; how
  * they are split depends on the shapes and lengths alone, so equal calls give equal bits.

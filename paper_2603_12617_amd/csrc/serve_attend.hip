@@ -56,6 +56,11 @@ template <> __device__ __forceinline__ f16v mfma<_Float16>(u4 a, u4 b, f16v c)
 {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(h8, a), __builtin_bit_cast(h8, b), c, 0, 0, 0);
 }
+// Weights are powers of two times 2^kLift.  The largest is at most 2^8 (the maximum that they are relative to may lag by that); float16 holds up to
+// 2^15.9 and nothing below 2^-25, so of a lift of 7 no weight is too large, and those between 2^-25 and 2^-32 of the largest still count: without it 131072
+// keys of 2^-25.02 beside one of 1 were 0 in the values' sum but not in the weights', 0.4 % of the result.  bfloat16 has the range of float32.
+template <typename T> constexpr float kLift = 0.f;
+template <> constexpr float kLift<_Float16> = 7.f;
 // two floats rounded to nearest even
 template <typename T> __device__ __forceinline__ unsigned pack(float x, float y);
 template <> __device__ __forceinline__ unsigned pack<__bf16>(float x, float y) { const f2 f = {x, y}; return __builtin_bit_cast(unsigned, __builtin_convertvector(f, b2)); }
@@ -506,7 +511,7 @@ __global__ void __launch_bounds__(64 * kRows * kKeys, DK > 192 || (kRows == 1 &&
     for (int d = 0; d < kD; ++d)
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[d][r] = 0.f;
-    float top = -INFINITY, sum = 0.f;                        // of the row, powers of two; sum: of this half's keys
+    float top = -INFINITY, sum = 0.f;                        // of the row: what weights are relative to (powers of two); sum: of this half's keys
 
     auto work = [&](int t, int buf) {
         const int key0 = t * KT;
@@ -565,10 +570,11 @@ __global__ void __launch_bounds__(64 * kRows * kKeys, DK > 192 || (kRows == 1 &&
             for (int r = 0; r < 16; ++r) most = fmaxf(most, s[n][r]);
         const f2 both = halves(most);
         most = fmaxf(both[0], both[1]) * p.scale;
-        // the weights are taken relative to a maximum that lags behind by at most a factor of 2^8 (row by row: what a row gets does not depend on its neighbours)
-        const bool behind = most > top + 8.f;
+        // the weights are taken relative to a maximum that lags behind by at most a factor of 2^8 (row by row: what a row gets does not depend on its neighbours),
+        // less the lift: `top` is that, so that all that is rescaled or joined has one exact reference
+        const bool behind = most > top + (8.f + kLift<T>);
         if (__any(behind)) {
-            const float now = behind ? most : top, back = behind ? __builtin_amdgcn_exp2f(top - now) : 1.f;
+            const float now = behind ? most - kLift<T> : top, back = behind ? __builtin_amdgcn_exp2f(top - now) : 1.f;
             top = now;
             sum *= back;
 #pragma unroll

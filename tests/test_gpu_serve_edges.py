@@ -160,3 +160,34 @@ def test_new_tokens_beyond_32_bits_stay_in_the_arrays():
     got = G._run_pages(st, 16, tokens=20)
     assert got["cu"].tolist() == [0, 5, 0x7fffffff, 0x7fffffff, 0x7fffffff] and got["kv"].tolist() == [8, 3, 3, 9] and got["nfree"].tolist() == [1]
     assert got["pos"].tolist() == [3, 4, 5, 6, 7] + [-1] * 15 and got["slot"][:5].tolist() == [67, 68, 69, 70, 71] and (got["slot"][5:] == -1).all()
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("Bn,rows,heads,D", [(64, 1, 8, 80), (4, 130, 64, 64)])
+def test_attention_small_weights_beside_a_large_one(dtype, Bn, rows, heads, D):
+    """One key far above 131072 equal ones, each of them less than 2^-25 of it and 0.4 % together; all values are 1.  Whole requests of one
+    token and chunks, both so many that keys are not split (which would bring the others to parts of their own)."""
+    torch = _torch()
+    n, page = 262144, 64
+    k = torch.zeros((n // page, page, heads, D), dtype=G._dt(dtype), device=DEV)
+    v = torch.ones_like(k)
+    tail = (torch.arange(page, device=DEV) & 4) != 0
+    k[:, ~tail, :, 0] = -1000.0                             # (weight 0: half of the keys, so that the small weights' sum, in float32, is not theirs)
+    k[0, 0, :, 0] = 17.34375
+    gap = float(k[0, 0, 0, 0])
+    q = torch.zeros((Bn * rows, heads, D), dtype=k.dtype, device=DEV)
+    q[:, :, 0] = 8.0
+    table = torch.arange(n // page, dtype=torch.int32, device=DEV).expand(Bn, -1).contiguous()     # (all requests on the same pages)
+    out, lse = torch.empty_like(q), torch.empty(q.shape[:2], device=DEV)
+    ws = torch.empty(B.sd_attend_workspace_bytes(q, k, table), dtype=torch.uint8, device=DEV)
+    print("case", dtype, Bn, rows, heads, D, flush=True)
+    B.sd_attend(q, k, v, G._i32(np.arange(Bn + 1) * rows), G._i32([n] * Bn), table, out, 0.125, lse=lse, ws=ws)
+    torch.cuda.synchronize()
+    # Weights and the result are rounded once each, relative; weights below float16's normal numbers to 2^-25 of a scale on which the largest is
+    # at least 2^7; values are added up 16 keys at a time, each sum of about 1 rounded or cut to 24 bits.
+    tol = 2.1 * G.UNIT[dtype] + n * 2.0 ** -32 + n / 16 * 2.0 ** -23
+    assert float((out.double() - 1.0).abs().max()) <= tol
+    pos = n - rows + np.arange(rows)
+    seen = (pos + 1) // 8 * 4 + np.maximum((pos + 1) % 8 - 4, 0)
+    want = gap + np.log1p(seen * np.exp(-gap))
+    assert np.abs(lse.double().cpu().numpy().reshape(Bn, rows, heads) - want[None, :, None]).max() <= gap * 2.0 ** -22 + 1e-5
