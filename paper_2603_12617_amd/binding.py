@@ -418,7 +418,7 @@ def sd_acceptance(p, q, acc_out, stream=None) -> None:
 
 # ---------------------------------------------------------------------------
 # A served verification step (include/specdec.h): tables, cache, attention, verification from logits.
-# Tensors may be views: whatever strides the C ABI takes are passed on.
+# Tensors may be views: whatever strides the C ABI takes are passed on.  Calls go to torch's current stream unless one is given.
 # A call of a small step takes as long as its checks here, so these are few and plain: an array's type, its number of
 # entries, that it is whole and on the GPU.
 _SD_DTYPE = {}
@@ -426,8 +426,15 @@ _SD_DTYPE = {}
 
 def _sd_types():
     import torch
-    _SD_DTYPE.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2, "i32": torch.int32, "f32": torch.float32})
+    _SD_DTYPE.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2, "i32": torch.int32, "f32": torch.float32,
+                      "stream": torch._C._cuda_getCurrentRawStream})
     return _SD_DTYPE
+
+
+def _sd_stream(stream, t):
+    """Address of the stream of a call: the one given, or torch's current one of the tensor's device, on which the torch
+    operations before and behind the call run.  (Asked for by its address: torch.cuda.current_stream() takes 1 to 3 us, this 0.1.)"""
+    return _SD_DTYPE["stream"](t.get_device()) if stream is None else stream.cuda_stream
 
 
 def _sd_dtype(t) -> int:
@@ -473,7 +480,7 @@ def sd_pages(pages, length, add, table, free, nfree, page, pages_out, length_out
                       _rows(table, "table", i32, (B, width)), _want(free, "free", i32, pool), pages_out.data_ptr(), length_out.data_ptr(),
                       kv_out.data_ptr(), nfree_out.data_ptr(), _want(cu_out, "cu_out", i32, B + 1), _want(slot_out, "slot_out", i32, T),
                       _want(pos_out, "pos_out", i32, T))
-    rc = lib().sd_pages(C.byref(step), _stream_ptr(stream))
+    rc = lib().sd_pages(C.byref(step), _sd_stream(stream, table))
     if rc != 0:
         raise SdError(rc, "sd_pages")
 
@@ -495,7 +502,7 @@ def sd_cache_store(k, v, slot, k_cache, v_cache, stream=None) -> None:
     T = slot.numel()
     shape, ks, vs = (T, heads, D), k.stride(), v.stride()
     rc = lib().sd_cache_store(C.byref(c), _rows(k, "k", dtype, shape), ks[0], ks[1], _rows(v, "v", dtype, shape), vs[0], vs[1],
-                              _want(slot, "slot", _SD_DTYPE["i32"], T), T, _stream_ptr(stream))
+                              _want(slot, "slot", _SD_DTYPE["i32"], T), T, _sd_stream(stream, k_cache))
     if rc != 0:
         raise SdError(rc, "sd_cache_store")
 
@@ -521,7 +528,7 @@ def sd_attend(q, k_cache, v_cache, cu, kv, table, out, scale, *, lse=None, windo
     a = SdAttention(c, B, T, Hq, width, table.stride(0) if B > 1 else width, _rows(q, "q", dtype, shape), qs[0], qs[1],
                     _rows(out, "out", dtype, shape), os[0], os[1], None if lse is None else _want(lse, "lse", _SD_DTYPE["f32"], T * Hq),
                     _want(cu, "cu", i32, B + 1), _want(kv, "kv", i32, B), _rows(table, "table", i32, (B, width)), window, scale)
-    rc = lib().sd_attend(C.byref(a), _dptr(ws), ws.numel() * ws.element_size(), _stream_ptr(stream))
+    rc = lib().sd_attend(C.byref(a), _dptr(ws), ws.numel() * ws.element_size(), _sd_stream(stream, q))
     if rc != 0:
         raise SdError(rc, "sd_attend")
 
@@ -547,6 +554,6 @@ def sd_verify_logits(p, q, tok, r, noise, tau, cu, n_out, next_out, ws, stream=N
                  _want(tok, "tok", i32, N), _want(r, "r", f32, N), _rows(noise, "noise", f32, (B, V)),
                  noise.stride(0) if B > 1 else V, _want(tau, "tau", f32, B), _want(cu, "cu", i32, B + 1))
     rc = lib().sd_verify_logits(C.byref(a), _want(n_out, "n_out", i32, B), _want(next_out, "next_out", i32, B), _dptr(ws),
-                                ws.numel() * ws.element_size(), _stream_ptr(stream))
+                                ws.numel() * ws.element_size(), _sd_stream(stream, p))
     if rc != 0:
         raise SdError(rc, "sd_verify_logits")

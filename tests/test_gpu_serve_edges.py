@@ -191,3 +191,24 @@ def test_attention_small_weights_beside_a_large_one(dtype, Bn, rows, heads, D):
     seen = (pos + 1) // 8 * 4 + np.maximum((pos + 1) % 8 - 4, 0)
     want = gap + np.log1p(seen * np.exp(-gap))
     assert np.abs(lse.double().cpu().numpy().reshape(Bn, rows, heads) - want[None, :, None]).max() <= gap * 2.0 ** -22 + 1e-5
+
+
+def test_calls_follow_the_torch_operations_before_them():
+    """Inside a stream's block the operators wait for what torch computes there, and torch for them."""
+    torch = _torch()
+    b = G._Batch([5, 33, 1], [900, 400, 2000], 8, 2, 128, 16, "bf16", seed=12)
+    want, _ = b.gpu()
+    q, k, v, table, cu, kv = b.q.to(DEV), b.k.to(DEV), b.v.to(DEV), G._i32(b.table), G._i32(b.cu), G._i32(b.kv)
+    ws = torch.empty(B.sd_attend_workspace_bytes(q, k, table), dtype=torch.uint8, device=DEV)
+    late, out, copy = torch.zeros_like(q), torch.zeros_like(q), torch.zeros_like(q)
+    busy = torch.randn((4096, 4096), device=DEV)
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        for _ in range(20):
+            busy = torch.tanh(busy @ busy)                  # (some milliseconds)
+        late.copy_(q)
+        B.sd_attend(late, k, v, cu, kv, table, out, b.scale, ws=ws)
+        copy.copy_(out)
+    torch.cuda.synchronize()
+    assert torch.equal(copy, want)
