@@ -212,3 +212,60 @@ def test_calls_follow_the_torch_operations_before_them():
         copy.copy_(out)
     torch.cuda.synchronize()
     assert torch.equal(copy, want)
+
+
+def test_a_whole_step_replays_from_a_graph():
+    """Tables, cache writes, attention and verification, captured on torch's current stream."""
+    torch = _torch()
+    Bn, page, Hq, Hkv, D, k, V = 3, 16, 8, 2, 64, 4, 20000
+    rng = np.random.default_rng(5)
+    g = torch.Generator(device=DEV).manual_seed(5)
+    st = G._pages_state(rng, Bn, page, 40, 30, 500, 5, held_extra=1)
+    i = {n: G._i32(x) for n, x in st.items()}
+    T, pool = Bn * (k + 1), len(st["free"])
+    new = lambda *s: torch.full(s, -7, dtype=torch.int32, device=DEV)  # noqa: E731
+    o = dict(pages=new(Bn), length=new(Bn), kv=new(Bn), nfree=new(1), cu=new(Bn + 1), slot=new(T), pos=new(T), n=new(Bn), next=new(Bn),
+             table=i["table"], free=i["free"])
+    bf = lambda *s: torch.randn(s, generator=g, device=DEV).to(torch.bfloat16)  # noqa: E731
+    o["k"], o["v"], q = bf(pool, page, Hkv, D), bf(pool, page, Hkv, D), bf(T, Hq, D)
+    o["out"], o["lse"], acc, kn, vn = torch.empty_like(q), torch.empty((T, Hq), device=DEV), new(Bn), bf(T, Hkv, D), bf(T, Hkv, D)
+    d = {n: x if x is None else torch.as_tensor(x).to(DEV) for n, x in G._logits(rng, [k] * Bn, V, "bf16").items()}
+    ws = torch.empty(B.sd_attend_workspace_bytes(q, o["k"], i["table"]), dtype=torch.uint8, device=DEV)
+    vws = torch.empty(B.sd_verify_logits_workspace_bytes(d["p"], d["q"], d["tau"]), dtype=torch.uint8, device=DEV)
+
+    def step():
+        B.sd_pages(i["pages"], i["length"], i["add"], i["table"], i["free"], i["nfree"], page, o["pages"], o["length"], o["kv"], o["nfree"], o["cu"],
+                   o["slot"], o["pos"], accepted=acc)
+        B.sd_cache_store(kn, vn, o["slot"], o["k"], o["v"])
+        B.sd_attend(q, o["k"], o["v"], o["cu"], o["kv"], i["table"], o["out"], D ** -0.5, lse=o["lse"], ws=ws)
+        B.sd_verify_logits(d["p"], d["q"], d["tok"], d["r"], d["noise"], d["tau"], o["cu"], o["n"], o["next"], vws)
+
+    acc.fill_(0)
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for turn in range(5):
+        acc.copy_(G._i32(rng.integers(-1, k + 1, Bn)))
+        for x in (q, kn, vn):
+            x.copy_(bf(*x.shape))
+        d["r"].uniform_(0.0, 1.0)
+        before = {n: o[n].clone() for n in ("k", "v", "table", "free")}
+        for n in ("pages", "length", "kv", "nfree", "cu", "slot", "pos", "n", "next", "out", "lse"):
+            o[n].fill_(-7)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = {n: x.clone() for n, x in o.items()}
+        for n, x in before.items():
+            o[n].copy_(x)
+        step()
+        torch.cuda.synchronize()
+        for n, x in o.items():
+            assert torch.equal(got[n], x), (turn, n)
+        want = SO.pages(accepted=acc.tolist(), page=page, **{**st, "nfree": 30})
+        for n in ("pages", "length", "kv", "cu", "slot", "pos", "nfree"):
+            assert got[n].tolist() == want[n].tolist(), (turn, n)
+        assert all(got["table"][b, :m].tolist() == want["table"][b, :m].tolist() for b, m in enumerate(want["pages"]))
+        assert (got["out"] != -7).all() and (got["n"] >= 0).all() and (got["next"] >= 0).all()
