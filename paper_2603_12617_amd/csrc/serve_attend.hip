@@ -290,6 +290,7 @@ __device__ __forceinline__ bool unit_of(const Attend &p, int x, int rows, int ke
     int per = longest;                                       // nothing is split
     if (p.once || p.level) {
         const int n = total(tiles);
+        if (n == 0) return false;                            // no request has a row
         all = total(all);
         const int least = min(max(p.min_steps, (longest + kMaxParts - 1) / kMaxParts), longest);   // (a row is joined from at most kMaxParts)
         if (n < p.once) {
@@ -306,7 +307,7 @@ __device__ __forceinline__ bool unit_of(const Attend &p, int x, int rows, int ke
         }
         // What is more than twice as long as the mean is split in any case.
         if (p.level && p.units > n)
-            per = min(per, max(max((int)(all / (float)(p.units - n)) + 1, (int)(2.f * all / (float)max(n, 1))), least));
+            per = min(per, max(max((int)(all / (float)(p.units - n)) + 1, (int)(2.f * all / (float)n)), least));
         per = __builtin_amdgcn_readfirstlane(per);
     }
     auto splits_of = [&](const Work &v) { return max((v.steps + per - 1) / per, 1); };

@@ -269,3 +269,19 @@ def test_a_whole_step_replays_from_a_graph():
             assert got[n].tolist() == want[n].tolist(), (turn, n)
         assert all(got["table"][b, :m].tolist() == want["table"][b, :m].tolist() for b, m in enumerate(want["pages"]))
         assert (got["out"] != -7).all() and (got["n"] >= 0).all() and (got["next"] >= 0).all()
+
+
+@pytest.mark.parametrize("Bn,width", [(1, 8), (1, 40), (1, 600), (2, 600), (70, 600)])
+def test_attention_of_requests_without_rows(Bn, width):
+    """An idle step: no request has a token, the batch is padded.  Nothing is written."""
+    torch = _torch()
+    q = torch.ones((5, 8, 64), dtype=torch.bfloat16, device=DEV)
+    k = torch.ones((20, 16, 2, 64), dtype=torch.bfloat16, device=DEV)
+    out, lse = torch.full_like(q, -7.0), torch.full((5, 8), -7.0, device=DEV)
+    table = torch.zeros((Bn, width), dtype=torch.int32, device=DEV)
+    ws = torch.full((B.sd_attend_workspace_bytes(q, k, table),), 0x01, dtype=torch.uint8, device=DEV)
+    print("case", Bn, width, flush=True)
+    for kv in (0, 16 * width):
+        B.sd_attend(q, k, k, G._i32([0] * (Bn + 1)), G._i32([kv] * Bn), table, out, 0.125, lse=lse, ws=ws)
+        torch.cuda.synchronize()
+        assert (out == -7).all() and (lse == -7).all()
