@@ -895,48 +895,54 @@ int64_t part_rows(const sd_attention &a, const Plan &p) { return p.many ? (int64
 // parts, (maximum, sum) of each, and where a row's parts are
 size_t part_bytes(const sd_attention &a, const Plan &p) { return p.join ? (size_t)part_rows(a, p) * (a.cache.D + 2) * 4 + (size_t)a.tokens * a.Hq * sizeof(int4) : 0; }
 
-template <typename T, int DK, bool kFull, int kRows, int kKeys, int KT, bool kUnits> void launch_shape(const Attend &p, dim3 grid, hipStream_t st)
+template <typename T, int DK, bool kFull, int kRows, int kKeys, int KT, bool kUnits> hipError_t launch_shape(const Attend &p, dim3 grid, hipStream_t st)
 {
     constexpr int tiles = kKeys * 4 * KT * Shape<DK>::kPitch, bytes = tiles + (kRows == 1 ? 4 * kIds * kKeys : 0);
     static_assert(kKeys == 1 || kKeys * (64 + 32 * (DK + 4)) * 4 <= tiles, "the join has room");
     const auto kernel = sd_attend_kernel<T, DK, kFull, kRows, kKeys, KT, kUnits>;
-    static const hipError_t once = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    (void)once;
+    if (bytes > 64 * 1024) {                                 // (each call: it is the current device's)
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        if (e != hipSuccess) return e;
+    }
     hipLaunchKernelGGL(kernel, grid, dim3(64 * kRows * kKeys), bytes, st, p);
+    return hipGetLastError();
 }
-template <typename T, int DK, bool kFull> void launch(const Attend &p, const Plan &plan, hipStream_t st)
+template <typename T, int DK, bool kFull> hipError_t launch(const Attend &p, const Plan &plan, hipStream_t st)
 {
     const int64_t heads = p.a.cache.heads, items = (int64_t)plan.tiles * plan.splits;
     const dim3 grid((unsigned)(!plan.many ? ((int64_t)plan.units + 7) / 8 * 8 * heads : plan.grouped ? items * ((heads + 7) / 8 * 8) : items * heads));
     // (shared tiles of 64 and 32 keys, 8 x 512 tokens over 2048 keys, D = 64: 88 and 98 us, 128: 140 and 150, 192, where 64 leave no room for a second workgroup: 236 and
     // 213, 256, where 32 do not either, the accumulators being so many: 306 and 370)
     constexpr int KT = DK != 192 ? 64 : 32;
-    if (plan.many) launch_shape<T, DK, kFull, 4, 1, KT, false>(p, grid, st);
-    else if (plan.rows == 128) launch_shape<T, DK, kFull, 4, 1, KT, true>(p, grid, st);
-    else if constexpr (kFull && DK <= 128) launch_shape<T, DK, kFull, 1, 2, 32, true>(p, grid, st);
-    if (plan.join) {
+    hipError_t e = hipErrorInvalidValue;
+    if (plan.many) e = launch_shape<T, DK, kFull, 4, 1, KT, false>(p, grid, st);
+    else if (plan.rows == 128) e = launch_shape<T, DK, kFull, 4, 1, KT, true>(p, grid, st);
+    else if constexpr (kFull && DK <= 128) e = launch_shape<T, DK, kFull, 1, 2, 32, true>(p, grid, st);
+    if (e == hipSuccess && plan.join) {
         const int64_t rows = p.a.tokens * p.a.Hq;
         // (few rows are as long as one's chain of parts: 1 token over 8000 keys 16.8 us by workgroups, 23.5 by wavefronts; 2560 rows over 2000 keys 38 and 35)
         if (rows <= 1024) hipLaunchKernelGGL((sd_join_kernel<T, 256>), dim3((unsigned)rows), dim3(256), 0, st, p);
         else hipLaunchKernelGGL((sd_join_kernel<T, 64>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, p);
+        e = hipGetLastError();
     }
+    return e;
 }
-template <typename T, int DK> void launch(const Attend &p, const Plan &plan, hipStream_t st)
+template <typename T, int DK> hipError_t launch(const Attend &p, const Plan &plan, hipStream_t st)
 {
     // (a head of 96 or 192 fills its row of products, but not the 128 or 256 elements from row to row in LDS)
     if constexpr (2 * DK == Shape<DK>::kPitch) {
-        if (p.a.cache.D == DK) { launch<T, DK, true>(p, plan, st); return; }
+        if (p.a.cache.D == DK) return launch<T, DK, true>(p, plan, st);
     }
-    launch<T, DK, false>(p, plan, st);
+    return launch<T, DK, false>(p, plan, st);
 }
-template <typename T> void launch(const Attend &p, const Plan &plan, hipStream_t st)
+template <typename T> hipError_t launch(const Attend &p, const Plan &plan, hipStream_t st)
 {
     switch (plan.dk) {
-        case 64: launch<T, 64>(p, plan, st); break;
-        case 96: launch<T, 96>(p, plan, st); break;
-        case 128: launch<T, 128>(p, plan, st); break;
-        case 192: launch<T, 192>(p, plan, st); break;
-        default: launch<T, 256>(p, plan, st); break;
+        case 64: return launch<T, 64>(p, plan, st);
+        case 96: return launch<T, 96>(p, plan, st);
+        case 128: return launch<T, 128>(p, plan, st);
+        case 192: return launch<T, 192>(p, plan, st);
+        default: return launch<T, 256>(p, plan, st);
     }
 }
 
@@ -986,9 +992,8 @@ int sd_attend(const sd_attention *args, void *ws, size_t ws_bytes, void *hip_str
     p.info = plan.join ? static_cast<int4 *>(ws) : nullptr;
     p.part = reinterpret_cast<float *>(static_cast<int4 *>(ws) + (size_t)a.tokens * a.Hq);
     p.part_ml = p.part + parts * a.cache.D;
-    if (a.cache.dtype == SD_BF16) launch<__bf16>(p, plan, static_cast<hipStream_t>(hip_stream));
-    else launch<_Float16>(p, plan, static_cast<hipStream_t>(hip_stream));
-    return hipGetLastError() == hipSuccess ? SD_OK : SD_EHIP;
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    return (a.cache.dtype == SD_BF16 ? launch<__bf16>(p, plan, st) : launch<_Float16>(p, plan, st)) == hipSuccess ? SD_OK : SD_EHIP;
 }
 
 }  // extern "C"

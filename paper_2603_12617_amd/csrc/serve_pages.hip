@@ -204,9 +204,9 @@ extern "C" int sd_pages(const sd_page_step *step, void *hip_stream)
     int64_t grid = (s.tokens + 1023) / 1024;
     grid = grid < 1 ? 1 : grid > 1024 ? 1024 : grid;
     const unsigned bytes = (unsigned)s.B * 5 * sizeof(int);
-    static const hipError_t once = hipFuncSetAttribute(reinterpret_cast<const void *>(sd_pages_kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
-                                                       SD_MAX_REQUESTS * 5 * sizeof(int));
-    (void)once;
+    if (bytes > 64 * 1024 &&                                  // (each call: it is the current device's)
+        hipFuncSetAttribute(reinterpret_cast<const void *>(sd_pages_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != hipSuccess)
+        return SD_EHIP;
     hipLaunchKernelGGL(sd_pages_kernel, dim3((unsigned)grid), dim3(kThreads), bytes, static_cast<hipStream_t>(hip_stream), p);
     return hipGetLastError() == hipSuccess ? SD_OK : SD_EHIP;
 }
