@@ -161,6 +161,7 @@ int sd_cache_store(const sd_cache *cache, const void *k, int64_t k_tok_stride, i
  * before they multiply the values (in float16 those below 2^-21 of a row's largest lose bits, and below 2^-32 they vanish there, though not
  * from the sum that divides).  D a multiple of 8, at most SD_MAX_HEAD_DIM; rows of D elements and all
  * strides 16-byte aligned.
+ * Refused with SD_EUNSUPPORTED: more threads than a launch holds, 2^32 (thousands of requests with thousands of key heads each).
  * `ws` (16-byte aligned) needs sd_attend_workspace_bytes.  It holds parts of rows whose keys are split over workgroups; how
  * they are split depends on the shapes and lengths alone, so equal calls give equal bits.
  */
@@ -195,6 +196,7 @@ int sd_attend(const sd_attention *a, void *ws, size_t ws_bytes, void *hip_stream
  * next[b] = that of row n; r, q and noise are not used.
  * A logit that is NaN counts as -inf (probability 0), +inf as the largest float.  A row without any finite logit
  * has all probabilities 0, and gives next = 0.  tok is clamped to [0, V).
+ * Rows of p and q together fewer than 2^24.
  * Sums are float64 over float32 parts, in a fixed order.  ws (16-byte aligned): sd_verify_logits_workspace_bytes.
  */
 typedef struct {

@@ -891,6 +891,20 @@ Plan plan_of(const sd_attention &a)
     p.join = p.once || p.level;
     return p;
 }
+// workgroups of the first launch
+int64_t groups(const sd_attention &a, const Plan &p)
+{
+    const int64_t heads = a.cache.heads, items = (int64_t)p.tiles * p.splits;
+    return !p.many ? ((int64_t)p.units + 7) / 8 * 8 * heads : p.grouped ? items * ((heads + 7) / 8 * 8) : items * heads;
+}
+// lanes of a row of the second: few rows are as long as one's chain of parts (1 token over 8000 keys 16.8 us by workgroups, 23.5 by wavefronts; 2560 rows over 2000 keys 38 and 35)
+int64_t join_lanes(const sd_attention &a) { return a.tokens * a.Hq <= 1024 ? 256 : 64; }
+// whether a launch can have so many threads
+bool fits(const sd_attention &a, const Plan &p)
+{
+    const int64_t most = 0xffffffffll;
+    return groups(a, p) * (p.rows == 128 ? 256 : 128) <= most && (!p.join || (a.tokens * a.Hq + 3) * join_lanes(a) <= most);
+}
 int64_t part_rows(const sd_attention &a, const Plan &p) { return p.many ? (int64_t)p.splits * a.tokens * a.Hq : (int64_t)p.units * a.cache.heads * p.rows; }
 // parts, (maximum, sum) of each, and where a row's parts are
 size_t part_bytes(const sd_attention &a, const Plan &p) { return p.join ? (size_t)part_rows(a, p) * (a.cache.D + 2) * 4 + (size_t)a.tokens * a.Hq * sizeof(int4) : 0; }
@@ -909,8 +923,7 @@ template <typename T, int DK, bool kFull, int kRows, int kKeys, int KT, bool kUn
 }
 template <typename T, int DK, bool kFull> hipError_t launch(const Attend &p, const Plan &plan, hipStream_t st)
 {
-    const int64_t heads = p.a.cache.heads, items = (int64_t)plan.tiles * plan.splits;
-    const dim3 grid((unsigned)(!plan.many ? ((int64_t)plan.units + 7) / 8 * 8 * heads : plan.grouped ? items * ((heads + 7) / 8 * 8) : items * heads));
+    const dim3 grid((unsigned)groups(p.a, plan));
     // (shared tiles of 64 and 32 keys, 8 x 512 tokens over 2048 keys, D = 64: 88 and 98 us, 128: 140 and 150, 192, where 64 leave no room for a second workgroup: 236 and
     // 213, 256, where 32 do not either, the accumulators being so many: 306 and 370)
     constexpr int KT = DK != 192 ? 64 : 32;
@@ -920,8 +933,7 @@ template <typename T, int DK, bool kFull> hipError_t launch(const Attend &p, con
     else if constexpr (kFull && DK <= 128) e = launch_shape<T, DK, kFull, 1, 2, 32, true>(p, grid, st);
     if (e == hipSuccess && plan.join) {
         const int64_t rows = p.a.tokens * p.a.Hq;
-        // (few rows are as long as one's chain of parts: 1 token over 8000 keys 16.8 us by workgroups, 23.5 by wavefronts; 2560 rows over 2000 keys 38 and 35)
-        if (rows <= 1024) hipLaunchKernelGGL((sd_join_kernel<T, 256>), dim3((unsigned)rows), dim3(256), 0, st, p);
+        if (join_lanes(p.a) == 256) hipLaunchKernelGGL((sd_join_kernel<T, 256>), dim3((unsigned)rows), dim3(256), 0, st, p);
         else hipLaunchKernelGGL((sd_join_kernel<T, 64>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, p);
         e = hipGetLastError();
     }
@@ -953,7 +965,8 @@ extern "C" {
 size_t sd_attend_workspace_bytes(const sd_attention *a)
 {
     if (!a || check(*a) != SD_OK) return 0;
-    return 16 + part_bytes(*a, plan_of(*a));
+    const Plan plan = plan_of(*a);
+    return fits(*a, plan) ? 16 + part_bytes(*a, plan) : 0;
 }
 
 int sd_attend(const sd_attention *args, void *ws, size_t ws_bytes, void *hip_stream)
@@ -962,12 +975,13 @@ int sd_attend(const sd_attention *args, void *ws, size_t ws_bytes, void *hip_str
     const sd_attention &a = *args;
     const int rc = check(a);
     if (rc != SD_OK) return rc;
+    const Plan plan = plan_of(a);
+    if (!fits(a, plan)) return SD_EUNSUPPORTED;
     if (!a.cache.k || !a.cache.v || !a.cu || !a.kv || !a.table || !ws) return SD_EINVAL;
     if (a.tokens > 0 && (!a.q || !a.out)) return SD_EINVAL;
     if (misaligned(a.cache.k, 16) || misaligned(a.cache.v, 16) || misaligned(a.q, 16) || misaligned(a.out, 16) || misaligned(a.lse, 4) ||
         misaligned(a.cu, 4) || misaligned(a.kv, 4) || misaligned(a.table, 4) || misaligned(ws, 16))
         return SD_EINVAL;
-    const Plan plan = plan_of(a);
     if (ws_bytes < 16 + part_bytes(a, plan)) return SD_ENOMEM;
     if (a.tokens == 0) return SD_OK;
     Attend p;

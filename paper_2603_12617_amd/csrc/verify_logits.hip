@@ -415,16 +415,18 @@ __global__ void __launch_bounds__(kThreads) sd_draw_kernel(const sd_logits s, co
 
 bool misaligned(const void *p, unsigned a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
 
+int64_t stat_rows(const sd_logits &s) { return s.rows + (s.q ? s.rows - s.B : 0); }
+
 int check(const sd_logits &s)
 {
     if (s.B <= 0 || s.V <= 0 || s.rows < s.B || s.p_stride < s.V || s.noise_stride < s.V) return SD_EINVAL;
     if (s.dtype != SD_F32 && s.dtype != SD_BF16 && s.dtype != SD_F16) return SD_EINVAL;
     if (s.q && s.rows > s.B && s.q_stride < s.V) return SD_EINVAL;
     if (s.V > SD_MAX_V || s.B > SD_MAX_REQUESTS || s.rows > (1 << 24)) return SD_EUNSUPPORTED;
+    if (stat_rows(s) * kThreads > 0xffffffffll) return SD_EUNSUPPORTED;      // (threads of a launch)
     return SD_OK;
 }
 int segments(const sd_logits &s) { return (int)((s.V + kSeg - 1) / kSeg); }
-int64_t stat_rows(const sd_logits &s) { return s.rows + (s.q ? s.rows - s.B : 0); }
 size_t race_bytes(const sd_logits &s) { return (size_t)s.B * sizeof(Race); }
 
 template <typename T> void launch(const sd_logits &s, Stat *stat, Race *race, int32_t *n, int32_t *next, hipStream_t st)

@@ -98,3 +98,16 @@ def test_shared_memory_beyond_64k_is_asked_for_on_every_call(launches):
     calls = [("sd_attend",) + _heads(64), ("sd_pages", None, dict(B=64))]
     for call, seen in zip(calls, launches(*calls)):
         assert all(rc == 0 and attributes == 0 and kernels[0][1] <= 65536 for rc, attributes, kernels in seen), (call, seen)
+
+
+def test_launches_of_more_threads_than_fit_are_refused(launches):
+    """A launch has fewer than 2^32 threads a dimension: what needs more is refused, what does not is launched."""
+    wide = dict(heads=8192, D=64, page=1, k_page_stride=8192 * 64, v_page_stride=8192 * 64, k_tok_stride=8192 * 64, v_tok_stride=8192 * 64, k_head_stride=64, v_head_stride=64)
+    batch = dict(B=2000, tokens=2000, Hq=8192, width=4, table_stride=4, q_tok_stride=8192 * 64, out_tok_stride=8192 * 64)
+    rows = dict(B=4000, V=8, p_stride=8, q_stride=8, noise_stride=8)
+    calls = [("sd_attend", wide, dict(batch)), ("sd_attend", wide, dict(batch, B=4096, tokens=4096)), ("sd_attend", wide, dict(batch, B=4096, tokens=4096 * 40)),
+             ("sd_verify_logits", None, dict(rows, q=None, rows=(1 << 24) - 1)), ("sd_verify_logits", None, dict(rows, q=None, rows=1 << 24)),
+             ("sd_verify_logits", None, dict(rows, rows=(1 << 23) + 2000 - 1)), ("sd_verify_logits", None, dict(rows, rows=(1 << 23) + 2000))]
+    for (call, (rc, _, kernels)), fits in zip(((c, s[0]) for c, s in zip(calls, launches(*calls))), (True, False, False, True, False, True, False)):
+        assert rc == (0 if fits else -2) and bool(kernels) == fits, (call, rc, kernels)
+        assert all(0 < threads < 1 << 32 for threads, _ in kernels), (call, kernels)
