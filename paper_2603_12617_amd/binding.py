@@ -466,6 +466,13 @@ def _rows(t, name, dtype, shape):
     return t.data_ptr()
 
 
+def _room(ws):
+    """Device address and bytes of a workspace."""
+    if ws is None or not ws.is_cuda or not ws.is_contiguous():
+        raise ValueError("ws: a contiguous GPU tensor is wanted: got %s" % ("none" if ws is None else "%s %s" % (ws.dtype, list(ws.shape))))
+    return ws.data_ptr(), ws.numel() * ws.element_size()
+
+
 def sd_pages(pages, length, add, table, free, nfree, page, pages_out, length_out, kv_out, nfree_out, cu_out, slot_out, pos_out, *,
              accepted=None, stream=None) -> None:
     """Block tables and slot maps of a step.  pages, length, add, accepted [B] i32; table [B][width] i32 and free [pool] i32 are
@@ -528,7 +535,7 @@ def sd_attend(q, k_cache, v_cache, cu, kv, table, out, scale, *, lse=None, windo
     a = SdAttention(c, B, T, Hq, width, table.stride(0) if B > 1 else width, _rows(q, "q", dtype, shape), qs[0], qs[1],
                     _rows(out, "out", dtype, shape), os[0], os[1], None if lse is None else _want(lse, "lse", _SD_DTYPE["f32"], T * Hq),
                     _want(cu, "cu", i32, B + 1), _want(kv, "kv", i32, B), _rows(table, "table", i32, (B, width)), window, scale)
-    rc = lib().sd_attend(C.byref(a), _dptr(ws), ws.numel() * ws.element_size(), _sd_stream(stream, q))
+    rc = lib().sd_attend(C.byref(a), *_room(ws), _sd_stream(stream, q))
     if rc != 0:
         raise SdError(rc, "sd_attend")
 
@@ -553,7 +560,7 @@ def sd_verify_logits(p, q, tok, r, noise, tau, cu, n_out, next_out, ws, stream=N
                  None if q is None else _rows(q, "q", dtype, (N, V)), V if N < 2 or q is None else q.stride(0),
                  _want(tok, "tok", i32, N), _want(r, "r", f32, N), _rows(noise, "noise", f32, (B, V)),
                  noise.stride(0) if B > 1 else V, _want(tau, "tau", f32, B), _want(cu, "cu", i32, B + 1))
-    rc = lib().sd_verify_logits(C.byref(a), _want(n_out, "n_out", i32, B), _want(next_out, "next_out", i32, B), _dptr(ws),
-                                ws.numel() * ws.element_size(), _sd_stream(stream, p))
+    rc = lib().sd_verify_logits(C.byref(a), _want(n_out, "n_out", i32, B), _want(next_out, "next_out", i32, B), *_room(ws),
+                                _sd_stream(stream, p))
     if rc != 0:
         raise SdError(rc, "sd_verify_logits")

@@ -76,3 +76,13 @@ def test_calls_go_to_the_current_stream(library, name):
     assert library.calls[name][-1] == 0x1234
     _calls(stream=_Stream)[name]()
     assert library.calls[name][-1] == 0x5678
+
+
+@pytest.mark.parametrize("ws", [None, torch.zeros(64, dtype=torch.uint8), _On(torch.zeros((8, 16), dtype=torch.uint8)[:, :8])])
+def test_workspaces_that_are_refused(library, ws):
+    """A workspace on the host, or one that is not whole: a refusal, not an assertion, which optimised Python leaves out."""
+    with pytest.raises(ValueError):
+        B.sd_attend(_bf16(5, 4, 64), _bf16(8, 16, 2, 64), _bf16(8, 16, 2, 64), _i32(3), _i32(2), _i32(2, 4), _bf16(5, 4, 64), 0.125, ws=ws)
+    with pytest.raises(ValueError):
+        B.sd_verify_logits(_f32(5, 9), _f32(3, 9), _i32(3), _f32(3), _f32(2, 9), _f32(2), _i32(3), _i32(2), _i32(2), ws)
+    assert not library.calls
