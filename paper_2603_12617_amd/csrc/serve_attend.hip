@@ -987,7 +987,7 @@ int sd_attend(const sd_attention *args, void *ws, size_t ws_bytes, void *hip_str
     Attend p;
     p.a = a;
     p.G = (int)(a.Hq / a.cache.heads);
-    p.scale = (float)(a.scale * 1.4426950408889634);
+    p.scale = fmaxf((float)(a.scale * 1.4426950408889634), 1.2e-38f);    // (not 0: a masked score is -inf and has to stay that)
     // key / page for keys below 2^31: with s = ceil(log2(page)), floor(key m / 2^(31 + s)), m = floor(2^(31 + s) / page) + 1 <= 2^32 - 1
     int s = 0;
     while ((1ll << s) < a.cache.page) ++s;

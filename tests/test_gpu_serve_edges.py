@@ -285,3 +285,13 @@ def test_attention_of_requests_without_rows(Bn, width):
         B.sd_attend(q, k, k, G._i32([0] * (Bn + 1)), G._i32([kv] * Bn), table, out, 0.125, lse=lse, ws=ws)
         torch.cuda.synchronize()
         assert (out == -7).all() and (lse == -7).all()
+
+
+@pytest.mark.parametrize("new,kv", [([3], [40]), ([150], [400]), ([2], [3000])])
+@pytest.mark.parametrize("scale", [1e-30, 1e-38, 1e-42, 1e-300])
+def test_attention_scales_next_to_nothing(new, kv, scale):
+    """Scores that are 0 after scaling: the mean of the keys that a row sees."""
+    b = G._Batch(new, kv, 4, 2, 64, 16, "bf16", seed=2)
+    b.scale = scale
+    print("case", new, kv, scale, flush=True)
+    b.check()
