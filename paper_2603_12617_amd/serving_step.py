@@ -5,8 +5,8 @@
 The target is one attention layer with random weights between an embedding and an output projection, the draft a noisy copy of its
 output projection that looks at the last token alone.  Each step drafts k tokens per request, builds the block tables on the GPU (``sd_pages``), runs the chunk of
 last token and drafts through the target (``sd_cache_store``, ``sd_attend``), verifies the drafts from both models' logits (``sd_verify_logits``) and
-goes on from the accepted lengths.  Prompts enter the same way, as longer chunks without drafts.  Nothing is read back between the steps but
-the tokens, which are the program's result.
+goes on from the accepted lengths.  Prompts enter the same way, as longer chunks without drafts.  Nothing is read back between the steps: the
+tokens are the program's result, at its end.  A request whose table is full is refused from then on and emits no more.
 """
 import argparse
 
@@ -42,6 +42,7 @@ class Server:
         shape = (pool, page, target.Hkv, target.D)
         self.k, self.v = (torch.empty(shape, dtype=torch.bfloat16, device=self.dev) for _ in range(2))
         self.kv, self.cu = i32(requests), i32(requests + 1)
+        self.refused = torch.zeros(requests, dtype=torch.bool, device=self.dev)
         self.ws = torch.empty(16, dtype=torch.uint8, device=self.dev)
 
     def _workspace(self, n):
@@ -50,13 +51,15 @@ class Server:
         return self.ws
 
     def forward(self, tokens, add, accepted):
-        """The target's hidden rows behind a batch of chunks: `tokens` of all requests, add[b] of request b."""
+        """The target's hidden rows behind a batch of chunks: `tokens` of all requests, add[b] of request b.  Those of a request that
+        is refused for want of pages mean nothing: none of its chunk is in the cache, and its accepted length is -1 in the next step."""
         t, T = self.t, tokens.numel()
         slot, pos = (torch.empty(T, dtype=torch.int32, device=self.dev) for _ in range(2))
         a, b = self.now, self.then
         B.sd_pages(a["pages"], a["length"], add, self.table, self.free, a["nfree"], self.page, b["pages"], b["length"], self.kv, b["nfree"], self.cu, slot, pos,
                    accepted=accepted)
         self.now, self.then = b, a
+        self.refused = (self.kv == b["length"]) & (add > 0)
         x = t.embed[tokens.long()]
         qkv = (x @ t.qkv).view(T, t.Hq + 2 * t.Hkv, t.D)
         q, k, v = qkv[:, :t.Hq], qkv[:, t.Hq:t.Hq + t.Hkv], qkv[:, t.Hq + t.Hkv:]
@@ -72,11 +75,13 @@ class Server:
 
 
 def serve(requests=8, drafts=4, steps=6, prompt=50, vocab=32000, tau=0.8, seed=0, device="cuda:0"):
-    """Tokens of every request, and the accepted lengths of the steps [steps][requests] (both lists)."""
+    """Tokens of every request, and the accepted lengths of the steps [steps][requests] (both lists; -1: refused in that step)."""
     dev = torch.device(device)
     g = torch.Generator(device=dev).manual_seed(seed + 1)
     target = Target(vocab, 8, 2, 64, dev, seed)
     server = Server(target, requests, device=device)
+    if not 0 < prompt <= server.table.shape[1] * server.page:
+        raise ValueError("prompts of 1 to %d tokens are wanted: got %d" % (server.table.shape[1] * server.page, prompt))
     temp = torch.full((requests,), tau, device=dev)
     rand = lambda *s: torch.rand(s, generator=g, device=dev)  # noqa: E731
     race = lambda: torch.empty((requests, vocab), device=dev).exponential_(generator=g)  # noqa: E731
@@ -100,6 +105,7 @@ def serve(requests=8, drafts=4, steps=6, prompt=50, vocab=32000, tau=0.8, seed=0
         hidden = server.forward(tok.flatten(), add, accepted)
         q = torch.stack(logits, 1).view(requests * drafts, vocab) if drafts else None
         accepted, nxt = server.verify(hidden @ target.head, q, tok[:, 1:].flatten(), rand(requests * drafts), race(), temp)
+        accepted, nxt = torch.where(server.refused, -1, accepted), torch.where(server.refused, tok[:, 0], nxt)     # (where it was)
         step = torch.cat([tok[:, 1:], nxt[:, None]], 1)
         at = torch.arange(drafts + 1, device=dev)
         step = torch.where(at < accepted[:, None], step, torch.where(at == accepted[:, None], nxt[:, None], -1))
