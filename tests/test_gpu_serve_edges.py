@@ -295,3 +295,22 @@ def test_attention_scales_next_to_nothing(new, kv, scale):
     b.scale = scale
     print("case", new, kv, scale, flush=True)
     b.check()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("k,V", [([0], 7), ([1], 1), ([0, 3, 1, 8, 0], 4099), ([3] * 5, 8193), ([5, 70], 300), ([2, 2], 50257)])
+@pytest.mark.parametrize("draft", [True, False])
+def test_small_batches_leave_little_undecided(dtype, k, V, draft):
+    """Over many batches of few requests, nine in ten are compared: rounding could have decided otherwise only in the others."""
+    sure = all_of_them = 0
+    for seed in range(max(4, 40 // len(k)) if V < 10000 else 8):
+        d = G._logits(np.random.default_rng(1000 * seed + V), k, V, dtype, draft)
+        n, nx = G._run_verify(d)
+        host = lambda x: None if x is None else x.double().numpy()  # noqa: E731
+        wn, wx, close = SO.verify_logits(host(d["p"]), host(d["q"]), d["tok"], d["r"], d["noise"], d["tau"], d["cu"])
+        ok = close > 4e-5
+        assert np.array_equal(n[ok], wn[ok]) and np.array_equal(nx[ok], wx[ok]), (seed, n, wn, nx, wx, close)
+        sure += int(ok.sum())
+        all_of_them += len(k)
+    print("case", dtype, k, V, draft, "%d of %d" % (sure, all_of_them), flush=True)
+    assert sure > 0.9 * all_of_them
