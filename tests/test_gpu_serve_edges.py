@@ -314,3 +314,24 @@ def test_small_batches_leave_little_undecided(dtype, k, V, draft):
         all_of_them += len(k)
     print("case", dtype, k, V, draft, "%d of %d" % (sure, all_of_them), flush=True)
     assert sure > 0.9 * all_of_them
+
+
+@pytest.mark.parametrize("new,kv,D", [([1] * 64, list(range(200, 840, 10)), 128), ([5, 1], [300, 20], 256), ([150, 1], [400, 30], 256)])
+def test_attention_with_more_than_64k_of_shared_memory_replays_from_a_graph(new, kv, D):
+    """What such a launch asks the runtime for may be asked while a stream is captured."""
+    torch = _torch()
+    b = G._Batch(new, kv, 8, 8, D, 16, "bf16", seed=D)
+    want, want_lse = b.gpu()
+    q, k, v, table, cu, lengths = b.q.to(DEV), b.k.to(DEV), b.v.to(DEV), G._i32(b.table), G._i32(b.cu), G._i32(b.kv)
+    out, lse = torch.empty_like(q), torch.empty(q.shape[:2], device=DEV)
+    ws = torch.empty(B.sd_attend_workspace_bytes(q, k, table), dtype=torch.uint8, device=DEV)
+    torch.cuda.synchronize()
+    print("case", len(new), D, flush=True)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        B.sd_attend(q, k, v, cu, lengths, table, out, b.scale, lse=lse, ws=ws)
+    for _ in range(3):
+        out.fill_(-7.0), lse.fill_(-7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and torch.equal(lse, want_lse)
