@@ -8,9 +8,9 @@
 //           raced: score(x) = weight(x) / noise(x).  Workgroups of a request meet in a 64-bit maximum of
 //           (score's bits, lowest place), whose order does not matter; the last one writes n and next.
 //
-// Bound by the logits' way from HBM: 2 k + 1 rows a request in `stats`, two rows and the noise again in `draw`; beside it `stats` has
-// 32 clocks of vector instructions a logit and SIMD lane group (half of them the power of two).  256 requests of 4 drafts, V = 151936, bfloat16: 128 us for
-// 700 MB, 5.5 TB/s of the 6.1 that a pure read reaches, and 61 us for the draw's 289 MB, 4.7 TB/s behind a chain of dependent reads.  8 of 4,
+// Bound by the logits' way from HBM: 2 k + 1 rows a request in `stats`, two rows and the noise again in `draw`; beside it `stats` has 11 vector
+// instructions a logit (counted: 58 million of a wavefront for 350 million logits), one of them the power of two.  256 requests of 4 drafts, V = 151936,
+// bfloat16: 127 us for 700 MB, 5.5 TB/s of the 6.1 that a pure read reaches, and 62 us for the draw's 289 MB, 4.7 TB/s behind a chain of dependent reads.  8 of 4,
 // V = 32000, float: 4.8 and 7.8 us, the launch and such chains.
 //
 // The difference is taken before it is multiplied: of l c - top c each part would be rounded in units of its own size, which for masks of -1e10
@@ -265,6 +265,7 @@ __device__ __forceinline__ float less(float w, float v, float i)
 // a probability
 __device__ __forceinline__ float weight(float l, const Row &r, Heat h) { return power_any(clean(l), r.top, h) * r.inv; }
 
+// Scores are taken with the reciprocal instruction, which is off by a unit in the last place, less than a weight is; a division is a chain of about ten.
 // larger scores win, of equal ones the lowest place
 __device__ __forceinline__ u64 entry(float score, int x) { return ((u64)__float_as_uint(score) << 32) | (0xffffffffu - (unsigned)x); }
 __device__ __forceinline__ u64 larger(u64 a, u64 b) { return a > b ? a : b; }
