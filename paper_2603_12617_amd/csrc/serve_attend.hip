@@ -852,7 +852,7 @@ Plan plan_of(const sd_attention &a)
     p.rows = own ? 32 : 128;
     const int64_t step = p.dk != 192 ? 64 : 32;                                         // keys
     int64_t longest = a.width * a.cache.page;
-    if (a.window > 0 && a.window + p.rows / G + 1 < longest) longest = a.window + p.rows / G + 1;
+    if (a.window > 0 && a.window < longest && a.window + p.rows / G + 1 < longest) longest = a.window + p.rows / G + 1;
     // Short parts where workgroups are few and wait for nothing but their own keys (1 request, 1500 keys, parts of 64, 128, 256, 1024 keys at least: 11.4, 12.3,
     // 14.3, 26 us); where there are more, the room for workgroups ends the splitting first.
     p.min_steps = there >= 64 ? 4 : 1;

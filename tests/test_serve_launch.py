@@ -111,3 +111,12 @@ def test_launches_of_more_threads_than_fit_are_refused(launches):
     for (call, (rc, _, kernels)), fits in zip(((c, s[0]) for c, s in zip(calls, launches(*calls))), (True, False, False, True, False, True, False)):
         assert rc == (0 if fits else -2) and bool(kernels) == fits, (call, rc, kernels)
         assert all(0 < threads < 1 << 32 for threads, _ in kernels), (call, kernels)
+
+
+def test_a_window_beyond_all_keys_is_none(launches):
+    """Any window that reaches past the longest context, up to the largest number there is, launches what no window does."""
+    one = dict(B=1, tokens=1, width=256, table_stride=256)
+    few = dict(B=2, tokens=400, width=256, table_stride=256)
+    for batch in (one, few):
+        found = [seen[0] for seen in launches(*(("sd_attend", {}, dict(batch, window=w)) for w in (0, 4096, 1 << 40, (1 << 63) - 1, (1 << 63) - 20)))]
+        assert all(x == found[0] for x in found) and len(found[0][2]) == 2, found
